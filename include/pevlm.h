@@ -214,6 +214,82 @@ int pevlm_layer_forward(const pevlm_shape_t* shape, int32_t last_len, const void
                         void* o_question, float* lse_question, void* ws_prefill, size_t ws_prefill_bytes,
                         void* ws_query, size_t ws_query_bytes, void* stream);
 
+/* ---- A cache of many sequences: pages, and keys and values in 4 bits -------------------------------------------------
+ *
+ * (The paper has no counterpart: it stops at the cache of one video.  These calls are for a server that keeps several
+ * videos resident and answers questions about them, Eq. 5 over a cache in pages.)
+ *
+ * The tokens of a sequence live in pages of page_len tokens, found through its row of the page table: token t at slot
+ * page_table[sequence][t / page_len] * page_len + t % page_len.  Pages that no sequence holds stand on a free list, a stack of which the
+ * first *free_count entries count.  Lengths, tables, list and count are DEVICE int32, so that a step whose lengths only the GPU
+ * knows can be captured into a graph; int32 pointers need 4-byte alignment, `slots` and `positions` 16-byte.
+ */
+typedef struct {
+    int32_t num_pages; /* pages there are, num_pages * page_len < 2^31 */
+    int32_t page_len;  /* tokens of a page: 16, 32, 64 or 128 */
+    int32_t num_seqs;  /* sequences: rows of the page table */
+    int32_t max_pages; /* columns of the page table, max_pages * page_len <= 2^30 */
+} pevlm_pages_t;
+
+/*
+ * Gives the pages of finished sequences back: for every sequence r with finished[r] != 0, in order, its
+ * ceil(lens[r] / page_len) pages are pushed onto the free list, and its length becomes 0.
+ *   finished, lens [num_seqs], page_table [num_seqs, max_pages], free_count [1]: read
+ *   free_list [num_pages]: written from entry *free_count on; lens_out [num_seqs], free_count_out [1]: written
+ * Outputs must not be the inputs (PEVLM_EINVAL): a step goes lens -> release -> lens_out -> assign -> lens.  The page table
+ * stays as it is: what stands behind a sequence's length means nothing.  Lengths and counts outside their range count as the
+ * nearest one inside; nothing is written past the end of the free list.
+ */
+int pevlm_pages_release(const pevlm_pages_t* pages, const int32_t* finished, const int32_t* lens, const int32_t* page_table,
+                        int32_t* free_list, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out, void* stream);
+
+/*
+ * Room for new_lens[r] >= 0 more tokens of every sequence: pages taken from the top of the free list in the order of the
+ * sequences (the j-th page taken by all of them is free_list[*free_count - 1 - j]), and for each new token, the rows of all sequences
+ * one after another, its slot and its position.
+ *   lens, new_lens [num_seqs], free_list, free_count: read; page_table: entries of fresh pages written
+ *   lens_out [num_seqs] = lens + new_lens, free_count_out [1]
+ *   row_start [num_seqs + 1]: first row of each sequence, and the number of rows at the end
+ *   slots, positions [max_rows]: written in full, rows that no sequence has with slot -1 and position 0.  (positions is the pos_ids
+ *   of pevlm_rope_qk, slots those of pevlm_packed_store, lens_out and row_start those of pevlm_packed_attn.)
+ * A sequence whose pages run out (the free list, counted over all sequences up to this one, or its row of the table) or
+ * whose rows end past max_rows gets no pages: its rows have slot -1 and its lens_out stays lens.  One that needs no fresh page is never
+ * turned away for the list.  Outputs must not be the inputs (see pevlm_pages_release).  max_rows >= 0, <= 2^30.
+ */
+int pevlm_pages_assign(const pevlm_pages_t* pages, const int32_t* lens, const int32_t* new_lens, int32_t* page_table,
+                       const int32_t* free_list, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out,
+                       int32_t* row_start, int32_t* slots, int32_t* positions, int64_t max_rows, void* stream);
+
+/*
+ * The packed cache: K and V in groups of 16 values along the head, each value an e2m1 number (4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * and their negatives) times the e4m3 scale of its group; 4.5 bits a value.  For a group with largest magnitude m
+ *   scale = e4m3(clamp(m / 6, 2^-9, 448)),  value = e2m1(x / scale), both to nearest, halfway to the even code, the second saturating,
+ * so values up to 2688 are in range, and those of a group below 2^-9 * 6 share the smallest scale.  Every value of the cache is a
+ * bf16 and an fp16 number: reading it back rounds nothing.
+ *   cache [num_pages, Hkv, page_len / 16, 18 * d] bytes: per 16 tokens ("tile") of a page and kv head, token u = 8 h + k, element e:
+ *     K codes   byte u * d/2 + e/2                             (element 2i in the low half of its byte)
+ *     V codes   byte 8 d + ((h * 8 + c) * 8 + k) * d/16 + b      byte b of eighth c of the head (d/8 elements)
+ *     K scales  byte 16 d + k * 2n + (i / w) * 2w + h * w + i % w  group i < n = d/16, w = d/64
+ *     V scales  byte 17 d + i * 16 + (k / 2) * 4 + h * 2 + k % 2
+ * i.e. in the order in which the threads of the attention's matrix products hold them.
+ * pevlm_packed_cache_bytes: bytes of the whole cache (0 if shape or pages are invalid), 16-byte aligned.
+ * Of `shape` these calls use num_q_heads, num_kv_heads, head_dim and softmax_scale (and pevlm_packed_attn sink_len); batch must be 1.
+ */
+size_t pevlm_packed_cache_bytes(const pevlm_shape_t* shape, const pevlm_pages_t* pages);
+
+/*
+ * Writes rows into their slots: k, v [n_rows, Hkv, d] bf16, rows k_stride / v_stride elements apart (0 = Hkv * d; a multiple of 8, at
+ * least Hkv * d: rows of one projection's output can be taken where they stand), slots [n_rows].
+ * A row whose slot is outside [0, num_pages * page_len) is skipped.  Slots must differ: of a slot named twice the contents are a mix.
+ */
+int pevlm_packed_store(const pevlm_shape_t* shape, const pevlm_pages_t* pages, const void* k, const void* v, int64_t k_stride,
+                       int64_t v_stride, const int32_t* slots, int64_t n_rows, void* cache, void* stream);
+
+/* Reads rows back: k_out, v_out [n_rows, Hkv, d] bf16 receive what the cache holds at slots [n_rows] (any order, any of them more than
+ * once); zeros for a slot out of range. */
+int pevlm_packed_load(const pevlm_shape_t* shape, const pevlm_pages_t* pages, const void* cache, const int32_t* slots, int64_t n_rows,
+                      void* k_out, void* v_out, void* stream);
+
 /* Bytes of workspace the given call needs for this shape (0 if the shape is invalid). */
 size_t pevlm_workspace_bytes(const pevlm_shape_t* shape, int which /* pevlm_workspace_kind_t */);
 

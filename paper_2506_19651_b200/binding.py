@@ -25,7 +25,8 @@ NOALLOC_SCRATCH_BYTES = 32 << 20
 EXPORTS = ["pevlm_rope_qk", "pevlm_rope_qkv", "pevlm_layer_forward", "pevlm_rope_qk_mrope", "pevlm_parallel_prefill_attn", "pevlm_block_attn", "pevlm_assemble_kv", "pevlm_query_attn",
            "pevlm_query_attn_noalloc",
            "pevlm_workspace_bytes", "pevlm_read_status", "pevlm_selftest_wait_expiry", "pevlm_tile_stats", "pevlm_strerror",
-           "pevlm_last_cuda_error"]
+           "pevlm_last_cuda_error",
+           "pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_cache_bytes", "pevlm_packed_store", "pevlm_packed_load"]
 
 
 class Shape(C.Structure):
@@ -48,6 +49,15 @@ def make_shape(S, B, N, Q, Hq, Hkv, d, theta=1e4, scale=0.0, mask_mode=MASK_PEVL
     return Shape(batch, S, B, N, Q, Hq, Hkv, d, theta, scale, mask_mode)
 
 
+class Pages(C.Structure):
+    """pevlm_pages_t"""
+    _fields_ = [("num_pages", C.c_int32), ("page_len", C.c_int32), ("num_seqs", C.c_int32), ("max_pages", C.c_int32)]
+
+
+def make_pages(num_pages, page_len, num_seqs, max_pages) -> Pages:
+    return Pages(num_pages, page_len, num_seqs, max_pages)
+
+
 class PevlmError(RuntimeError):
     def __init__(self, code, where):
         self.code = code
@@ -66,7 +76,7 @@ def lib():
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2506_19651_b200.build` "
                                "(there is no CPU fallback)")
         l = C.CDLL(LIB_PATH)
-        vp, sp = C.c_void_p, C.POINTER(Shape)
+        vp, sp, gp = C.c_void_p, C.POINTER(Shape), C.POINTER(Pages)
         l.pevlm_rope_qk.argtypes = [sp, vp, vp, vp, vp, C.c_int64, C.c_int64, vp, vp]
         l.pevlm_rope_qkv.argtypes = [sp, vp, vp, vp, vp, vp, vp, C.c_int64, C.c_int64, vp, vp]
         l.pevlm_rope_qkv.restype = C.c_int
@@ -90,6 +100,14 @@ def lib():
         l.pevlm_strerror.argtypes = [C.c_int]
         l.pevlm_strerror.restype = C.c_char_p
         l.pevlm_last_cuda_error.restype = C.c_char_p
+        l.pevlm_pages_release.argtypes = [gp] + [vp] * 8
+        l.pevlm_pages_assign.argtypes = [gp] + [vp] * 10 + [C.c_int64, vp]
+        l.pevlm_packed_cache_bytes.argtypes = [sp, gp]
+        l.pevlm_packed_cache_bytes.restype = C.c_size_t
+        l.pevlm_packed_store.argtypes = [sp, gp, vp, vp, C.c_int64, C.c_int64, vp, C.c_int64, vp, vp]
+        l.pevlm_packed_load.argtypes = [sp, gp, vp, vp, C.c_int64, vp, vp, vp]
+        for name in ("pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_store", "pevlm_packed_load"):
+            getattr(l, name).restype = C.c_int
         for name in ("pevlm_rope_qk", "pevlm_parallel_prefill_attn", "pevlm_assemble_kv", "pevlm_query_attn",
                      "pevlm_read_status", "pevlm_tile_stats"):
             getattr(l, name).restype = C.c_int
@@ -140,6 +158,12 @@ def _address(shape):
     if not isinstance(shape, Shape):
         raise C.ArgumentError(f"expected a Shape, got {type(shape).__name__}")
     return C.addressof(shape)
+
+
+def _pages_address(pages):
+    if not isinstance(pages, Pages):
+        raise C.ArgumentError(f"expected Pages, got {type(pages).__name__}")
+    return C.addressof(pages)
 
 
 def _check(rc, where):
@@ -201,6 +225,32 @@ def pevlm_query_attn_noalloc(shape: Shape, q_question, k_cache, v_cache, o, lse)
     """Question attention for callers that cannot allocate device memory: no workspace argument,
     the partials go to the library's built-in scratch array (see include/pevlm.h for its limits)."""
     _check(_native().query_attn_noalloc(_address(shape), q_question, k_cache, v_cache, o, lse, _stream()), "pevlm_query_attn_noalloc")
+
+
+def pevlm_pages_release(pages: Pages, finished, lens, page_table, free_list, free_count, lens_out, free_count_out):
+    _check(_native().pages_release(_pages_address(pages), finished, lens, page_table, free_list, free_count, lens_out, free_count_out,
+                                   _stream()), "pevlm_pages_release")
+
+
+def pevlm_pages_assign(pages: Pages, lens, new_lens, page_table, free_list, free_count, lens_out, free_count_out, row_start, slots,
+                       positions, max_rows: int):
+    _check(_native().pages_assign(_pages_address(pages), lens, new_lens, page_table, free_list, free_count, lens_out, free_count_out,
+                                  row_start, slots, positions, max_rows, _stream()), "pevlm_pages_assign")
+
+
+def pevlm_packed_cache_bytes(shape: Shape, pages: Pages) -> int:
+    return int(lib().pevlm_packed_cache_bytes(C.byref(shape), C.byref(pages)))
+
+
+def pevlm_packed_store(shape: Shape, pages: Pages, k, v, slots, n_rows: int, cache, k_stride: int = 0, v_stride: int = 0):
+    """k_stride, v_stride: elements from one row of k and v to the next, 0 = the rows stand one after another."""
+    _check(_native().packed_store(_address(shape), _pages_address(pages), k, v, k_stride, v_stride, slots, n_rows, cache, _stream()),
+           "pevlm_packed_store")
+
+
+def pevlm_packed_load(shape: Shape, pages: Pages, cache, slots, n_rows: int, k_out, v_out):
+    _check(_native().packed_load(_address(shape), _pages_address(pages), cache, slots, n_rows, k_out, v_out, _stream()),
+           "pevlm_packed_load")
 
 
 def pevlm_selftest_wait_expiry(workspace, limit_ns: int):

@@ -23,11 +23,11 @@ int fail_with_text(int code, const char* text) {
     return code;
 }
 
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-static bool aligned32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
-static bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
+static bool aligned16(const void* p) { return aligned_to(p, 16); }
+static bool aligned32(const void* p) { return aligned_to(p, 32); }
+static bool aligned256(const void* p) { return aligned_to(p, 256); }
 
-static int check_shape(const pevlm_shape_t* s) {
+int check_shape(const pevlm_shape_t* s) {
     if (!s) return PEVLM_EINVAL;
     if (s->batch < 1 || s->sink_len < 0 || s->num_blocks < 0 || s->query_len < 0) return PEVLM_EINVAL;
     if (s->num_blocks > 0 && s->block_len < 1) return PEVLM_EINVAL;
@@ -48,7 +48,7 @@ static int64_t n_video(const pevlm_shape_t* s, int last_len = 0) {
 }
 
 // What a device is does not change: looked up once for each.
-static int check_device() {
+int check_device() {
     static std::atomic<uint64_t> good{0};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -116,7 +116,7 @@ static int make_tmap(CUtensorMap* m, const void* base, int64_t tokens, int heads
     return PEVLM_OK;
 }
 
-static float resolve_scale(const pevlm_shape_t* s) {
+float resolve_scale(const pevlm_shape_t* s) {
     return s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / sqrtf(static_cast<float>(s->head_dim));
 }
 

@@ -199,6 +199,34 @@ struct CopySegments {
     int32_t batch;
 };
 
+// Page tables and slots (pages_kernel.cu).
+struct AssignParams {
+    const int32_t *lens, *new_lens, *free_list, *free_count;
+    int32_t *page_table, *lens_out, *free_count_out, *row_start, *slots, *positions;
+    int64_t max_rows, rows_per_cta;  // rows_per_cta is set by launch_assign
+    int32_t num_pages, num_seqs, max_pages, page_shift;
+};
+struct ReleaseParams {
+    const int32_t *finished, *lens, *page_table, *free_count;
+    int32_t *free_list, *lens_out, *free_count_out;
+    int32_t num_pages, num_seqs, max_pages, page_shift;
+};
+cudaError_t launch_assign(AssignParams p, cudaStream_t stream);
+cudaError_t launch_release(const ReleaseParams& p, cudaStream_t stream);
+
+// Rows of K and V to and from a packed cache (packed_kernel.cu).
+struct PackedRows {
+    const __nv_bfloat16 *k, *v;  // store
+    __nv_bfloat16 *k_out, *v_out;  // load
+    uint8_t* cache;
+    const int32_t* slots;
+    int64_t k_stride, v_stride;  // elements from row to row
+    int64_t n_rows;
+    int32_t Hkv, n_slots, page_shift;
+};
+cudaError_t launch_packed_store(const PackedRows& p, int head_dim, cudaStream_t stream);
+cudaError_t launch_packed_load(const PackedRows& p, int head_dim, cudaStream_t stream);
+
 cudaError_t launch_rope(const RopeParams& p, int head_dim, cudaStream_t stream);
 // tokens of a group of such a call, heads of V counted (not part of the ABI: the tests ask for it)
 extern "C" int pevlm_rope_group_size(int64_t n_tokens, int heads, int head_dim);
@@ -221,6 +249,11 @@ int check_query_args(const pevlm_shape_t* s, const void* q_question, const void*
                      const void* o, const float* lse);
 cudaError_t launch_decode(const DecodeParams& p, int head_dim, cudaStream_t stream);
 cudaError_t launch_merge(const MergeParams& p, cudaStream_t stream);
+// argument checks shared by the host-side translation units
+int check_shape(const pevlm_shape_t* s);
+int check_device();
+float resolve_scale(const pevlm_shape_t* s);
+inline bool aligned_to(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 // error reporting shared by the host-side translation units: both record a text that
 // pevlm_last_cuda_error returns on the calling thread
 int cuda_fail(cudaError_t e, const char* what);      // returns PEVLM_ECUDA

@@ -1,0 +1,123 @@
+// C ABI of the calls on a cache of many sequences (pages, 4-bit keys and values): argument checking and launches.
+#include <cstring>
+
+#include "internal.h"
+
+namespace pevlm {
+
+static int check_pages(const pevlm_pages_t* g) {
+    if (!g || g->num_pages < 1 || g->num_seqs < 1 || g->max_pages < 1) return PEVLM_EINVAL;
+    if (g->page_len != 16 && g->page_len != 32 && g->page_len != 64 && g->page_len != 128) return PEVLM_EUNSUPPORTED;
+    if (static_cast<int64_t>(g->num_pages) * g->page_len >= 1ll << 31) return PEVLM_EINVAL;
+    if (static_cast<int64_t>(g->max_pages) * g->page_len > 1ll << 30 || g->num_seqs > 1 << 20) return PEVLM_EINVAL;
+    return PEVLM_OK;
+}
+
+static int page_shift(const pevlm_pages_t* g) { return __builtin_ctz(static_cast<unsigned>(g->page_len)); }
+
+// What the packed calls ask of a shape.
+static int check_packed(const pevlm_shape_t* s, const pevlm_pages_t* g) {
+    int rc = check_shape(s);
+    if (rc == PEVLM_OK) rc = check_pages(g);
+    if (rc != PEVLM_OK) return rc;
+    return s->batch == 1 && s->num_kv_heads <= 32767 ? PEVLM_OK : PEVLM_EUNSUPPORTED;  // kv heads: a dimension of the grids
+}
+
+}  // namespace pevlm
+
+using namespace pevlm;
+
+extern "C" {
+
+int pevlm_pages_release(const pevlm_pages_t* g, const int32_t* finished, const int32_t* lens, const int32_t* page_table,
+                        int32_t* free_list, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out, void* stream) {
+    int rc = check_pages(g);
+    if (rc != PEVLM_OK) return rc;
+    if (!finished || !lens || !page_table || !free_list || !free_count || !lens_out || !free_count_out) return PEVLM_EINVAL;
+    if (lens_out == lens || free_count_out == free_count) return PEVLM_EINVAL;
+    if (!aligned_to(finished, 4) || !aligned_to(lens, 4) || !aligned_to(page_table, 4) || !aligned_to(free_list, 4) ||
+        !aligned_to(free_count, 4) || !aligned_to(lens_out, 4) || !aligned_to(free_count_out, 4))
+        return PEVLM_EALIGN;
+    rc = check_device();
+    if (rc != PEVLM_OK) return rc;
+    ReleaseParams p{finished, lens, page_table, free_count, free_list, lens_out, free_count_out, g->num_pages, g->num_seqs, g->max_pages, page_shift(g)};
+    const cudaError_t e = launch_release(p, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? PEVLM_OK : cuda_fail(e, "release launch");
+}
+
+int pevlm_pages_assign(const pevlm_pages_t* g, const int32_t* lens, const int32_t* new_lens, int32_t* page_table,
+                       const int32_t* free_list, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out,
+                       int32_t* row_start, int32_t* slots, int32_t* positions, int64_t max_rows, void* stream) {
+    int rc = check_pages(g);
+    if (rc != PEVLM_OK) return rc;
+    if (max_rows < 0 || max_rows > 1ll << 30) return PEVLM_EINVAL;
+    if (!lens || !new_lens || !page_table || !free_list || !free_count || !lens_out || !free_count_out || !row_start) return PEVLM_EINVAL;
+    if (max_rows > 0 && (!slots || !positions)) return PEVLM_EINVAL;
+    if (lens_out == lens || lens_out == new_lens || free_count_out == free_count) return PEVLM_EINVAL;
+    if (!aligned_to(lens, 4) || !aligned_to(new_lens, 4) || !aligned_to(page_table, 4) || !aligned_to(free_list, 4) ||
+        !aligned_to(free_count, 4) || !aligned_to(lens_out, 4) || !aligned_to(free_count_out, 4) || !aligned_to(row_start, 4) ||
+        !aligned_to(slots, 16) || !aligned_to(positions, 16))
+        return PEVLM_EALIGN;
+    rc = check_device();
+    if (rc != PEVLM_OK) return rc;
+    AssignParams p{lens, new_lens, free_list, free_count, page_table, lens_out, free_count_out, row_start, slots, positions,
+                   max_rows, 0, g->num_pages, g->num_seqs, g->max_pages, page_shift(g)};
+    const cudaError_t e = launch_assign(p, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? PEVLM_OK : cuda_fail(e, "assign launch");
+}
+
+size_t pevlm_packed_cache_bytes(const pevlm_shape_t* s, const pevlm_pages_t* g) {
+    if (check_packed(s, g) != PEVLM_OK) return 0;
+    return static_cast<size_t>(g->num_pages) * s->num_kv_heads * (g->page_len / 16) * 18 * s->head_dim;
+}
+
+int pevlm_packed_store(const pevlm_shape_t* s, const pevlm_pages_t* g, const void* k, const void* v, int64_t k_stride,
+                       int64_t v_stride, const int32_t* slots, int64_t n_rows, void* cache, void* stream) {
+    int rc = check_packed(s, g);
+    if (rc != PEVLM_OK) return rc;
+    if (n_rows < 0 || n_rows > 1ll << 30) return PEVLM_EINVAL;
+    if (!cache || (n_rows > 0 && (!k || !v || !slots))) return PEVLM_EINVAL;
+    const int64_t row = static_cast<int64_t>(s->num_kv_heads) * s->head_dim;
+    if (k_stride == 0) k_stride = row;
+    if (v_stride == 0) v_stride = row;
+    if (n_rows > 1 && (k_stride < row || v_stride < row || k_stride > 1ll << 32 || v_stride > 1ll << 32)) return PEVLM_EINVAL;
+    if (!aligned_to(k, 16) || !aligned_to(v, 16) || !aligned_to(cache, 16) || !aligned_to(slots, 4) || k_stride % 8 || v_stride % 8) return PEVLM_EALIGN;
+    if (n_rows == 0) return PEVLM_OK;
+    rc = check_device();
+    if (rc != PEVLM_OK) return rc;
+    PackedRows p;
+    memset(&p, 0, sizeof(p));
+    p.k = static_cast<const __nv_bfloat16*>(k);
+    p.v = static_cast<const __nv_bfloat16*>(v);
+    p.k_stride = k_stride; p.v_stride = v_stride;
+    p.cache = static_cast<uint8_t*>(cache);
+    p.slots = slots;
+    p.n_rows = n_rows;
+    p.Hkv = s->num_kv_heads; p.n_slots = g->num_pages * g->page_len; p.page_shift = page_shift(g);
+    const cudaError_t e = launch_packed_store(p, s->head_dim, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? PEVLM_OK : cuda_fail(e, "packed store launch");
+}
+
+int pevlm_packed_load(const pevlm_shape_t* s, const pevlm_pages_t* g, const void* cache, const int32_t* slots, int64_t n_rows,
+                      void* k_out, void* v_out, void* stream) {
+    int rc = check_packed(s, g);
+    if (rc != PEVLM_OK) return rc;
+    if (n_rows < 0 || n_rows > 1ll << 30) return PEVLM_EINVAL;
+    if (!cache || (n_rows > 0 && (!k_out || !v_out || !slots))) return PEVLM_EINVAL;
+    if (!aligned_to(k_out, 16) || !aligned_to(v_out, 16) || !aligned_to(cache, 16) || !aligned_to(slots, 4)) return PEVLM_EALIGN;
+    if (n_rows == 0) return PEVLM_OK;
+    rc = check_device();
+    if (rc != PEVLM_OK) return rc;
+    PackedRows p;
+    memset(&p, 0, sizeof(p));
+    p.cache = static_cast<uint8_t*>(const_cast<void*>(cache));
+    p.slots = slots;
+    p.n_rows = n_rows;
+    p.k_out = static_cast<__nv_bfloat16*>(k_out);
+    p.v_out = static_cast<__nv_bfloat16*>(v_out);
+    p.Hkv = s->num_kv_heads; p.n_slots = g->num_pages * g->page_len; p.page_shift = page_shift(g);
+    const cudaError_t e = launch_packed_load(p, s->head_dim, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? PEVLM_OK : cuda_fail(e, "packed load launch");
+}
+
+}  // extern "C"

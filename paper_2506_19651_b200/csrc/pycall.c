@@ -94,10 +94,29 @@ BEGIN(layer_forward, 18)
     int64_t wqb = I(16); void* st = P(17);
 END(pevlm_layer_forward(s, (int32_t)last, q, k, v, qv, qq, kc, vc, ov, (float*)lv, oq, (float*)lq, wp, (size_t)wpb, wq, (size_t)wqb, st))
 
+/* The calls on pages: the first argument is the address of a pevlm_pages_t, or of a shape with the pages behind it. */
+BEGIN(pages_release, 9)
+    void *fin = P(1), *len = P(2), *tab = P(3), *fl = P(4), *fc = P(5), *lo = P(6), *fo = P(7), *st = P(8);
+END(pevlm_pages_release((const pevlm_pages_t*)s, fin, len, tab, fl, fc, lo, fo, st))
+
+BEGIN(pages_assign, 13)
+    void *len = P(1), *add = P(2), *tab = P(3), *fl = P(4), *fc = P(5), *lo = P(6), *fo = P(7), *rs = P(8), *sl = P(9), *ps = P(10);
+    int64_t rows = I(11); void* st = P(12);
+END(pevlm_pages_assign((const pevlm_pages_t*)s, len, add, tab, fl, fc, lo, fo, rs, sl, ps, rows, st))
+
+BEGIN(packed_store, 10)
+    void *g = P(1), *k = P(2), *v = P(3); int64_t ks = I(4), vs = I(5); void* sl = P(6); int64_t rows = I(7); void *c = P(8), *st = P(9);
+END(pevlm_packed_store(s, (const pevlm_pages_t*)g, k, v, ks, vs, sl, rows, c, st))
+
+BEGIN(packed_load, 8)
+    void *g = P(1), *c = P(2), *sl = P(3); int64_t rows = I(4); void *k = P(5), *v = P(6), *st = P(7);
+END(pevlm_packed_load(s, (const pevlm_pages_t*)g, c, sl, rows, k, v, st))
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(rope_qk), METHOD(rope_qkv), METHOD(rope_qk_mrope), METHOD(parallel_prefill_attn),
                                 METHOD(block_attn), METHOD(assemble_kv), METHOD(query_attn), METHOD(query_attn_noalloc),
-                                METHOD(layer_forward), {NULL, NULL, 0, NULL}};
+                                METHOD(layer_forward), METHOD(pages_release), METHOD(pages_assign),
+                                METHOD(packed_store), METHOD(packed_load), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pevlm_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__pevlm_call(void) {

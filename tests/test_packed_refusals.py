@@ -1,0 +1,115 @@
+"""The calls on pages and on the packed cache refuse bad arguments on the host, before anything is launched (no GPU here)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import packed_reference as R
+from paper_2506_19651_b200 import binding as pb
+from paper_2506_19651_b200 import build as pbuild
+
+
+@pytest.fixture(scope="module")
+def lib():
+    pbuild.build()
+    return pb.lib()
+
+
+def at(x):
+    return C.c_void_p(x)
+
+
+BAD_PAGES = [((0, 16, 1, 1), pb.PEVLM_EINVAL), ((4, 16, 0, 1), pb.PEVLM_EINVAL), ((4, 16, 1, 0), pb.PEVLM_EINVAL), ((4, 0, 1, 1), pb.PEVLM_EUNSUPPORTED),
+             ((4, 48, 1, 1), pb.PEVLM_EUNSUPPORTED), ((4, 256, 1, 1), pb.PEVLM_EUNSUPPORTED), ((2 ** 27, 16, 1, 1), pb.PEVLM_EINVAL),
+             ((4, 128, 1, 2 ** 23 + 1), pb.PEVLM_EINVAL), ((4, 16, 2 ** 20 + 1, 1), pb.PEVLM_EINVAL)]
+
+
+def test_pages(lib):
+    g = pb.make_pages(8, 16, 4, 2)
+    p = [at(4096 * (i + 1)) for i in range(12)]
+    release = [p[0], p[1], p[2], p[3], p[4], p[5], p[6]]
+    assign = [p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9]]
+    for fields, code in BAD_PAGES:
+        bad = pb.make_pages(*fields)
+        assert lib.pevlm_pages_release(C.byref(bad), *release, None) == code, fields
+        assert lib.pevlm_pages_assign(C.byref(bad), *assign, 8, None) == code, fields
+    assert lib.pevlm_pages_release(None, *release, None) == pb.PEVLM_EINVAL
+    for i in range(7):
+        a = list(release); a[i] = None
+        assert lib.pevlm_pages_release(C.byref(g), *a, None) == pb.PEVLM_EINVAL
+        a[i] = at(4098)
+        assert lib.pevlm_pages_release(C.byref(g), *a, None) == pb.PEVLM_EALIGN
+    for i in range(10):
+        a = list(assign); a[i] = None
+        assert lib.pevlm_pages_assign(C.byref(g), *a, 8, None) == pb.PEVLM_EINVAL
+        a[i] = at(4098)
+        assert lib.pevlm_pages_assign(C.byref(g), *a, 8, None) == pb.PEVLM_EALIGN
+    for i in (8, 9):  # written 16 bytes at a time
+        a = list(assign); a[i] = at(4100)
+        assert lib.pevlm_pages_assign(C.byref(g), *a, 8, None) == pb.PEVLM_EALIGN
+    # outputs that are inputs
+    a = list(release); a[5] = a[1]
+    assert lib.pevlm_pages_release(C.byref(g), *a, None) == pb.PEVLM_EINVAL
+    a = list(release); a[6] = a[4]
+    assert lib.pevlm_pages_release(C.byref(g), *a, None) == pb.PEVLM_EINVAL
+    for out, src in ((5, 0), (5, 1), (6, 4)):
+        a = list(assign); a[out] = a[src]
+        assert lib.pevlm_pages_assign(C.byref(g), *a, 8, None) == pb.PEVLM_EINVAL
+    for rows in (-1, 2 ** 30 + 1):
+        assert lib.pevlm_pages_assign(C.byref(g), *assign, rows, None) == pb.PEVLM_EINVAL
+
+
+def test_packed_rows(lib):
+    s, g = pb.make_shape(0, 1, 0, 1, 4, 2, 64), pb.make_pages(8, 16, 4, 2)
+    assert pb.pevlm_packed_cache_bytes(s, g) == 8 * 2 * 18 * 64
+    p = at(4096)
+    store = lambda s, g, k=p, v=p, ks=0, vs=0, sl=p, n=4, c=p: lib.pevlm_packed_store(C.byref(s), C.byref(g), k, v, ks, vs, sl, n, c, None)
+    load = lambda s, g, c=p, sl=p, n=4, k=p, v=p: lib.pevlm_packed_load(C.byref(s), C.byref(g), c, sl, n, k, v, None)
+    for fields, code in BAD_PAGES:
+        bad = pb.make_pages(*fields)
+        assert store(s, bad) == code and load(s, bad) == code and pb.pevlm_packed_cache_bytes(s, bad) == 0
+    for field, val, code in (("head_dim", 96, pb.PEVLM_EUNSUPPORTED), ("num_kv_heads", 3, pb.PEVLM_EINVAL), ("batch", 2, pb.PEVLM_EUNSUPPORTED),
+                             ("batch", 0, pb.PEVLM_EINVAL)):
+        bad = pb.make_shape(0, 1, 0, 1, 4, 2, 64)
+        setattr(bad, field, val)
+        assert store(bad, g) == code and load(bad, g) == code, field
+    for f in (store, load):
+        for name in ("k", "v", "sl", "c"):
+            assert f(s, g, **{name: None}) == pb.PEVLM_EINVAL
+            assert f(s, g, **{name: at(4098)}) == pb.PEVLM_EALIGN
+        assert f(s, g, n=-1) == pb.PEVLM_EINVAL and f(s, g, n=2 ** 30 + 1) == pb.PEVLM_EINVAL
+        assert f(s, g, n=0, k=None, v=None, sl=None) == pb.PEVLM_OK
+    assert store(s, g, ks=120) == pb.PEVLM_EINVAL and store(s, g, vs=-128) == pb.PEVLM_EINVAL
+    assert store(s, g, ks=132) == pb.PEVLM_EALIGN
+
+
+def test_binding_types():
+    s, g = pb.make_shape(0, 1, 0, 1, 4, 2, 64), pb.make_pages(8, 16, 4, 2)
+    with pytest.raises(C.ArgumentError):
+        pb.pevlm_packed_store(g, s, None, None, None, 0, None)
+    with pytest.raises(C.ArgumentError):
+        pb.pevlm_pages_release(s, *[None] * 7)
+
+
+def test_reference_quantiser():
+    """The tests' own quantiser: hand values, and never a better choice of code at its scale."""
+    x = np.zeros((1, 16)); x[0, :8] = [6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5]
+    codes, scale = R.quantise(x)
+    assert R.SCALES[scale[0, 0]] == 1.0 and codes[0, :8].tolist() == [7, 0, 2, 2, 4, 4, 6, 6]
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((64, 16)) * 2.0 ** rng.integers(-6, 7, (64, 1))
+    codes, scale = R.quantise(x)
+    y = R.dequantise(codes, scale)
+    s = R.SCALES[scale][:, :, None]
+    best = np.abs(np.abs(x)[:, :, None] - s * R.MAGNITUDES).min(-1)
+    assert np.array_equal(np.abs(x - y), best) and (np.sign(y) * np.sign(x) >= 0).all()
+
+
+def test_reference_allocator():
+    a = R.Allocator(6, 16, 3, 3)
+    table, free = np.full((3, 3), -1), np.array([0, 1, 2, 3, 4, 5])
+    lens, table, count, start, slots, pos = a.assign(np.array([0, 0, 0]), np.array([17, 1, 60]), table, free, 6, 100)
+    assert lens.tolist() == [17, 1, 0] and count == 3 and table[0, :2].tolist() == [5, 4] and table[1, 0] == 3
+    assert slots[:18].tolist() == list(range(80, 96)) + [64, 48] and (slots[18:] == -1).all() and start.tolist() == [0, 17, 18, 78]
+    lens, free, count = a.release([0, 1, 0], lens, table, free, count)
+    assert lens.tolist() == [17, 0, 0] and count == 4 and free[3] == 3
