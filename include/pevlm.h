@@ -290,6 +290,26 @@ int pevlm_packed_store(const pevlm_shape_t* shape, const pevlm_pages_t* pages, c
 int pevlm_packed_load(const pevlm_shape_t* shape, const pevlm_pages_t* pages, const void* cache, const int32_t* slots, int64_t n_rows,
                       void* k_out, void* v_out, void* stream);
 
+/*
+ * Attention of the last rows of every sequence over the packed cache [Eq. 5 for many sequences; single tokens, drafted tokens and
+ * question blocks in one call].  Sequence r has lens[r] keys in the cache and rows row_start[r] .. row_start[r + 1] - 1 of q; its i-th
+ * of n rows is its token lens[r] - n + i, whose own key is in the cache already, and sees the keys up to its own.  With window > 0
+ * only those of the last `window` positions (its own among them) and of the sequence's first sink_len tokens (shape); window = 0: all.
+ *   q [n_rows, Hq, d] bf16 roped, rows q_stride elements apart (0 = Hq * d); lens [num_seqs], row_start [num_seqs + 1], page_table: as
+ *   pevlm_pages_assign leaves them;  o [n_rows, Hq, d] bf16, lse [Hq, n_rows] fp32 (may be NULL), written
+ *   max_rows: most rows of one sequence, as the caller knows it (n_rows if not): chooses the kernel, a larger row count stays correct
+ * A row that sees no key (a length of 0, or fewer keys than rows) has output 0 and LSE -inf.  Keys in a page whose table entry is outside
+ * [0, num_pages) count as not there.  Rows of q that no sequence has are not read, and of o and lse not written.  Scores of finite rows are formed from fp16
+ * operands (the cache's values are exact in it) and summed in fp32, probabilities rounded to fp16.
+ * workspace: >= pevlm_packed_workspace_bytes(...) bytes, 256-byte aligned, needs no value; two calls at a time need two.
+ */
+int pevlm_packed_attn(const pevlm_shape_t* shape, const pevlm_pages_t* pages, int32_t window, const void* q, int64_t q_stride,
+                      const void* cache, const int32_t* page_table, const int32_t* lens, const int32_t* row_start, int64_t n_rows,
+                      int64_t max_rows, void* o, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of pevlm_packed_attn (0 if an argument is invalid). */
+size_t pevlm_packed_workspace_bytes(const pevlm_shape_t* shape, const pevlm_pages_t* pages, int64_t n_rows, int64_t max_rows);
+
 /* Bytes of workspace the given call needs for this shape (0 if the shape is invalid). */
 size_t pevlm_workspace_bytes(const pevlm_shape_t* shape, int which /* pevlm_workspace_kind_t */);
 

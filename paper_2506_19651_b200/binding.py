@@ -26,7 +26,8 @@ EXPORTS = ["pevlm_rope_qk", "pevlm_rope_qkv", "pevlm_layer_forward", "pevlm_rope
            "pevlm_query_attn_noalloc",
            "pevlm_workspace_bytes", "pevlm_read_status", "pevlm_selftest_wait_expiry", "pevlm_tile_stats", "pevlm_strerror",
            "pevlm_last_cuda_error",
-           "pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_cache_bytes", "pevlm_packed_store", "pevlm_packed_load"]
+           "pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_cache_bytes", "pevlm_packed_store", "pevlm_packed_load",
+           "pevlm_packed_attn", "pevlm_packed_workspace_bytes"]
 
 
 class Shape(C.Structure):
@@ -106,7 +107,10 @@ def lib():
         l.pevlm_packed_cache_bytes.restype = C.c_size_t
         l.pevlm_packed_store.argtypes = [sp, gp, vp, vp, C.c_int64, C.c_int64, vp, C.c_int64, vp, vp]
         l.pevlm_packed_load.argtypes = [sp, gp, vp, vp, C.c_int64, vp, vp, vp]
-        for name in ("pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_store", "pevlm_packed_load"):
+        l.pevlm_packed_attn.argtypes = [sp, gp, C.c_int32, vp, C.c_int64, vp, vp, vp, vp, C.c_int64, C.c_int64, vp, vp, vp, C.c_size_t, vp]
+        l.pevlm_packed_workspace_bytes.argtypes = [sp, gp, C.c_int64, C.c_int64]
+        l.pevlm_packed_workspace_bytes.restype = C.c_size_t
+        for name in ("pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_store", "pevlm_packed_load", "pevlm_packed_attn"):
             getattr(l, name).restype = C.c_int
         for name in ("pevlm_rope_qk", "pevlm_parallel_prefill_attn", "pevlm_assemble_kv", "pevlm_query_attn",
                      "pevlm_read_status", "pevlm_tile_stats"):
@@ -251,6 +255,17 @@ def pevlm_packed_store(shape: Shape, pages: Pages, k, v, slots, n_rows: int, cac
 def pevlm_packed_load(shape: Shape, pages: Pages, cache, slots, n_rows: int, k_out, v_out):
     _check(_native().packed_load(_address(shape), _pages_address(pages), cache, slots, n_rows, k_out, v_out, _stream()),
            "pevlm_packed_load")
+
+
+def pevlm_packed_workspace_bytes(shape: Shape, pages: Pages, n_rows: int, max_rows: int) -> int:
+    return int(lib().pevlm_packed_workspace_bytes(C.byref(shape), C.byref(pages), n_rows, max_rows))
+
+
+def pevlm_packed_attn(shape: Shape, pages: Pages, window: int, q, cache, page_table, lens, row_start, n_rows: int, max_rows: int, o, lse,
+                      workspace, q_stride: int = 0):
+    """q_stride: elements from one row of q to the next, 0 = the rows stand one after another."""
+    _check(_native().packed_attn(_address(shape), _pages_address(pages), window, q, q_stride, cache, page_table, lens, row_start, n_rows,
+                                 max_rows, o, lse, workspace, workspace.nbytes, _stream()), "pevlm_packed_attn")
 
 
 def pevlm_selftest_wait_expiry(workspace, limit_ns: int):

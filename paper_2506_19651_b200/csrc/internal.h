@@ -227,6 +227,24 @@ struct PackedRows {
 cudaError_t launch_packed_store(const PackedRows& p, int head_dim, cudaStream_t stream);
 cudaError_t launch_packed_load(const PackedRows& p, int head_dim, cudaStream_t stream);
 
+// Attention over the packed cache (packed_attn_kernel.cu).
+struct PackedAttnParams {
+    const __nv_bfloat16* q;  // rows q_stride elements apart
+    const uint8_t* cache;
+    const int32_t *page_table, *lens, *row_start;
+    __nv_bfloat16* o;        // [n_rows, Hq, d]
+    float* lse;              // [Hq, n_rows] or NULL
+    float* part;             // shares of units that cross from one CTA into the next, two places for each CTA
+    int64_t q_stride;
+    int32_t n_rows, num_seqs, num_pages, max_pages, page_shift;
+    int32_t Hq, Hkv, G;
+    int32_t window, sink;    // window = 0: none
+    Divisor div_g;
+    float scale_log2;        // softmax scale * log2(e)
+};
+size_t packed_attn_workspace_bytes(int head_dim);
+cudaError_t launch_packed_attn(const PackedAttnParams& p, int head_dim, int max_rows, cudaStream_t stream);
+
 cudaError_t launch_rope(const RopeParams& p, int head_dim, cudaStream_t stream);
 // tokens of a group of such a call, heads of V counted (not part of the ABI: the tests ask for it)
 extern "C" int pevlm_rope_group_size(int64_t n_tokens, int heads, int head_dim);

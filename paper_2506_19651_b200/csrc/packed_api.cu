@@ -120,4 +120,54 @@ int pevlm_packed_load(const pevlm_shape_t* s, const pevlm_pages_t* g, const void
     return e == cudaSuccess ? PEVLM_OK : cuda_fail(e, "packed load launch");
 }
 
+// n_rows rows of a call, at most max_rows of one sequence.
+static int check_rows(const pevlm_shape_t* s, int64_t n_rows, int64_t max_rows) {
+    if (n_rows < 0 || max_rows < 0 || max_rows > n_rows) return PEVLM_EINVAL;
+    return n_rows * (s->num_q_heads / s->num_kv_heads) <= 1ll << 30 ? PEVLM_OK : PEVLM_EINVAL;
+}
+
+size_t pevlm_packed_workspace_bytes(const pevlm_shape_t* s, const pevlm_pages_t* g, int64_t n_rows, int64_t max_rows) {
+    if (check_packed(s, g) != PEVLM_OK || check_rows(s, n_rows, max_rows) != PEVLM_OK) return 0;
+    return kStatusBytes + packed_attn_workspace_bytes(s->head_dim);
+}
+
+int pevlm_packed_attn(const pevlm_shape_t* s, const pevlm_pages_t* g, int32_t window, const void* q, int64_t q_stride, const void* cache,
+                      const int32_t* page_table, const int32_t* lens, const int32_t* row_start, int64_t n_rows, int64_t max_rows, void* o,
+                      float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_packed(s, g);
+    if (rc == PEVLM_OK) rc = check_rows(s, n_rows, max_rows);
+    if (rc != PEVLM_OK) return rc;
+    if (window < 0) return PEVLM_EINVAL;
+    if (!cache || !page_table || !lens || !row_start || (n_rows > 0 && (!q || !o))) return PEVLM_EINVAL;
+    const int64_t row = static_cast<int64_t>(s->num_q_heads) * s->head_dim;
+    if (q_stride == 0) q_stride = row;
+    if (n_rows > 1 && (q_stride < row || q_stride > 1ll << 32)) return PEVLM_EINVAL;
+    if (!aligned_to(q, 16) || !aligned_to(cache, 16) || !aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_to(row_start, 4) ||
+        !aligned_to(o, 32) || !aligned_to(lse, 16) || q_stride % 8)
+        return PEVLM_EALIGN;
+    if (!workspace || workspace_bytes < pevlm_packed_workspace_bytes(s, g, n_rows, max_rows)) return PEVLM_EWORKSPACE;
+    if (!aligned_to(workspace, 256)) return PEVLM_EALIGN;
+    if (n_rows == 0 || max_rows == 0) return PEVLM_OK;
+    rc = check_device();
+    if (rc != PEVLM_OK) return rc;
+    PackedAttnParams p;
+    memset(&p, 0, sizeof(p));
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.cache = static_cast<const uint8_t*>(cache);
+    p.page_table = page_table; p.lens = lens; p.row_start = row_start;
+    p.o = static_cast<__nv_bfloat16*>(o);
+    p.lse = lse;
+    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kStatusBytes);
+    p.q_stride = q_stride;
+    p.n_rows = static_cast<int32_t>(n_rows);
+    p.num_seqs = g->num_seqs; p.num_pages = g->num_pages; p.max_pages = g->max_pages; p.page_shift = page_shift(g);
+    p.Hq = s->num_q_heads; p.Hkv = s->num_kv_heads; p.G = p.Hq / p.Hkv;
+    p.window = window < 1 << 30 ? window : 1 << 30;  // no sequence is longer
+    p.sink = s->sink_len;
+    p.div_g = make_divisor(p.G);
+    p.scale_log2 = resolve_scale(s) * 1.4426950408889634f;
+    const cudaError_t e = launch_packed_attn(p, s->head_dim, static_cast<int>(max_rows), static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? PEVLM_OK : cuda_fail(e, "packed attention launch");
+}
+
 }  // extern "C"

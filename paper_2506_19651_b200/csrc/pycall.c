@@ -112,11 +112,16 @@ BEGIN(packed_load, 8)
     void *g = P(1), *c = P(2), *sl = P(3); int64_t rows = I(4); void *k = P(5), *v = P(6), *st = P(7);
 END(pevlm_packed_load(s, (const pevlm_pages_t*)g, c, sl, rows, k, v, st))
 
+BEGIN(packed_attn, 16)
+    void* g = P(1); int64_t window = I(2); void* q = P(3); int64_t qs = I(4); void *c = P(5), *tab = P(6), *len = P(7), *rs = P(8);
+    int64_t rows = I(9), most = I(10); void *o = P(11), *lse = P(12), *ws = P(13); int64_t wb = I(14); void* st = P(15);
+END(pevlm_packed_attn(s, (const pevlm_pages_t*)g, (int32_t)window, q, qs, c, tab, len, rs, rows, most, o, (float*)lse, ws, (size_t)wb, st))
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(rope_qk), METHOD(rope_qkv), METHOD(rope_qk_mrope), METHOD(parallel_prefill_attn),
                                 METHOD(block_attn), METHOD(assemble_kv), METHOD(query_attn), METHOD(query_attn_noalloc),
                                 METHOD(layer_forward), METHOD(pages_release), METHOD(pages_assign),
-                                METHOD(packed_store), METHOD(packed_load), {NULL, NULL, 0, NULL}};
+                                METHOD(packed_store), METHOD(packed_load), METHOD(packed_attn), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pevlm_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__pevlm_call(void) {

@@ -83,6 +83,36 @@ def test_packed_rows(lib):
     assert store(s, g, ks=132) == pb.PEVLM_EALIGN
 
 
+def test_packed_attn(lib):
+    s, g = pb.make_shape(0, 1, 0, 1, 4, 2, 64), pb.make_pages(8, 16, 4, 2)
+    p = at(4096)
+    size = pb.pevlm_packed_workspace_bytes(s, g, 8, 2)
+    assert size > 0
+    names = dict(window=0, q=p, qs=0, c=p, tab=p, lens=p, start=p, rows=8, most=2, o=p, lse=p, ws=p, wb=size)
+
+    def attn(s=s, g=g, **kw):
+        return lib.pevlm_packed_attn(C.byref(s), C.byref(g), *(dict(names, **kw)[n] for n in names), None)
+    for fields, code in BAD_PAGES:
+        bad = pb.make_pages(*fields)
+        assert attn(g=bad) == code and pb.pevlm_packed_workspace_bytes(s, bad, 8, 2) == 0
+    for field, val, code in (("head_dim", 96, pb.PEVLM_EUNSUPPORTED), ("num_kv_heads", 3, pb.PEVLM_EINVAL), ("batch", 2, pb.PEVLM_EUNSUPPORTED),
+                             ("softmax_scale", -1.0, pb.PEVLM_EINVAL), ("sink_len", -1, pb.PEVLM_EINVAL)):
+        bad = pb.make_shape(0, 1, 0, 1, 4, 2, 64)
+        setattr(bad, field, val)
+        assert attn(s=bad) == code, field
+    for name in ("q", "c", "tab", "lens", "start", "o"):
+        assert attn(**{name: None}) == pb.PEVLM_EINVAL, name
+        assert attn(**{name: at(4098)}) == pb.PEVLM_EALIGN, name
+    assert attn(lse=at(4100)) == pb.PEVLM_EALIGN and attn(o=at(4096 + 16)) == pb.PEVLM_EALIGN
+    assert attn(window=-1) == pb.PEVLM_EINVAL
+    assert attn(qs=248) == pb.PEVLM_EINVAL and attn(qs=260) == pb.PEVLM_EALIGN
+    for rows, most in ((-1, 0), (8, 9), (8, -1), (2 ** 30, 1)):
+        assert attn(rows=rows, most=most) == pb.PEVLM_EINVAL
+        assert pb.pevlm_packed_workspace_bytes(s, g, rows, most) == 0
+    assert attn(ws=None) == pb.PEVLM_EWORKSPACE and attn(wb=size - 1) == pb.PEVLM_EWORKSPACE and attn(ws=at(4096 + 128)) == pb.PEVLM_EALIGN
+    assert attn(rows=0, most=0, q=None, o=None) == pb.PEVLM_OK
+
+
 def test_binding_types():
     s, g = pb.make_shape(0, 1, 0, 1, 4, 2, 64), pb.make_pages(8, 16, 4, 2)
     with pytest.raises(C.ArgumentError):
