@@ -214,6 +214,24 @@ int pevlm_layer_forward(const pevlm_shape_t* shape, int32_t last_len, const void
                         void* o_question, float* lse_question, void* ws_prefill, size_t ws_prefill_bytes,
                         void* ws_query, size_t ws_query_bytes, void* stream);
 
+/*
+ * Attention under a sliding window beside the first tokens, which stay visible (the streaming use of Sec. 5 by tokens instead of blocks):
+ * rows [first_token, first_token + n_tokens) of a sequence against its keys; row p sees key j <= p if j > p - window (its own position
+ * counts) or j < sink_len (of shape).  One call serves a whole prefill (first_token = 0), a chunk of one behind a cache, and single
+ * tokens (few rows take a kernel of their own, like those of pevlm_query_attn).
+ *   q [n_tokens, Hq, d] roped; k_cache, v_cache [cache_rows, Hkv, d], of which rows [0, first_token + n_tokens) may be read
+ *   (cache_rows >= that); o [n_tokens, Hq, d], lse [Hq, n_tokens] (may be NULL)
+ * batch > 1: sequences of equal lengths, n_tokens rows of q and o, cache_rows rows of the caches apart.  Of `shape` batch, sink_len, the head
+ * counts, head_dim and softmax_scale are used.  window >= 1; first_token + n_tokens <= 2^30.
+ * workspace: >= pevlm_window_workspace_bytes(...) bytes, 256-byte aligned; that of a call does for any first_token and window.
+ */
+int pevlm_window_attn(const pevlm_shape_t* shape, int32_t window, const void* q, const void* k_cache, const void* v_cache,
+                      int64_t first_token, int64_t n_tokens, int64_t cache_rows, void* o, float* lse, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of pevlm_window_attn (0 if an argument is invalid). */
+size_t pevlm_window_workspace_bytes(const pevlm_shape_t* shape, int32_t window, int64_t first_token, int64_t n_tokens);
+
 /* ---- A cache of many sequences: pages, and keys and values in 4 bits -------------------------------------------------
  *
  * (The paper has no counterpart: it stops at the cache of one video.  These calls are for a server that keeps several

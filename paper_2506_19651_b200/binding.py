@@ -27,7 +27,7 @@ EXPORTS = ["pevlm_rope_qk", "pevlm_rope_qkv", "pevlm_layer_forward", "pevlm_rope
            "pevlm_workspace_bytes", "pevlm_read_status", "pevlm_selftest_wait_expiry", "pevlm_tile_stats", "pevlm_strerror",
            "pevlm_last_cuda_error",
            "pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_cache_bytes", "pevlm_packed_store", "pevlm_packed_load",
-           "pevlm_packed_attn", "pevlm_packed_workspace_bytes"]
+           "pevlm_packed_attn", "pevlm_packed_workspace_bytes", "pevlm_window_attn", "pevlm_window_workspace_bytes"]
 
 
 class Shape(C.Structure):
@@ -110,6 +110,10 @@ def lib():
         l.pevlm_packed_attn.argtypes = [sp, gp, C.c_int32, vp, C.c_int64, vp, vp, vp, vp, C.c_int64, C.c_int64, vp, vp, vp, C.c_size_t, vp]
         l.pevlm_packed_workspace_bytes.argtypes = [sp, gp, C.c_int64, C.c_int64]
         l.pevlm_packed_workspace_bytes.restype = C.c_size_t
+        l.pevlm_window_attn.argtypes = [sp, C.c_int32, vp, vp, vp, C.c_int64, C.c_int64, C.c_int64, vp, vp, vp, C.c_size_t, vp]
+        l.pevlm_window_attn.restype = C.c_int
+        l.pevlm_window_workspace_bytes.argtypes = [sp, C.c_int32, C.c_int64, C.c_int64]
+        l.pevlm_window_workspace_bytes.restype = C.c_size_t
         for name in ("pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_store", "pevlm_packed_load", "pevlm_packed_attn"):
             getattr(l, name).restype = C.c_int
         for name in ("pevlm_rope_qk", "pevlm_parallel_prefill_attn", "pevlm_assemble_kv", "pevlm_query_attn",
@@ -229,6 +233,15 @@ def pevlm_query_attn_noalloc(shape: Shape, q_question, k_cache, v_cache, o, lse)
     """Question attention for callers that cannot allocate device memory: no workspace argument,
     the partials go to the library's built-in scratch array (see include/pevlm.h for its limits)."""
     _check(_native().query_attn_noalloc(_address(shape), q_question, k_cache, v_cache, o, lse, _stream()), "pevlm_query_attn_noalloc")
+
+
+def pevlm_window_workspace_bytes(shape: Shape, window: int, first_token: int, n_tokens: int) -> int:
+    return int(lib().pevlm_window_workspace_bytes(C.byref(shape), window, first_token, n_tokens))
+
+
+def pevlm_window_attn(shape: Shape, window: int, q, k_cache, v_cache, first_token: int, n_tokens: int, cache_rows: int, o, lse, workspace):
+    _check(_native().window_attn(_address(shape), window, q, k_cache, v_cache, first_token, n_tokens, cache_rows, o, lse, workspace,
+                                 workspace.nbytes, _stream()), "pevlm_window_attn")
 
 
 def pevlm_pages_release(pages: Pages, finished, lens, page_table, free_list, free_count, lens_out, free_count_out):

@@ -624,7 +624,8 @@ static int decode(const pevlm_shape_t* s, const QueryPlan& qp, const void* q, co
     AttnParams a = common_params(s);
     a.n_splits = qp.n_splits;
     DecodeParams p;
-    p.Q = a.Q; p.L = a.L; p.n_video = a.n_video; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.G;
+    memset(&p, 0, sizeof(p));
+    p.Q = a.Q; p.L = p.kv_rows = a.L; p.n_video = a.n_video; p.Hq = a.Hq; p.Hkv = a.Hkv; p.G = a.G;
     p.pieces = qp.pieces; p.pieces_per_split = qp.pieces_per_split; p.n_splits = qp.n_splits;
     p.scale = a.scale; p.scale_log2 = a.scale_log2;
     p.hdr = static_cast<WorkspaceHeader*>(workspace);
@@ -731,6 +732,121 @@ int pevlm_layer_forward(const pevlm_shape_t* s, int32_t last_len, const void* q,
     const cudaError_t e = launch_attn(p, d, m, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e, "attention launch");
     return Q > 0 && p.n_splits > 1 ? merge_question(p, d, p.o_question, p.lse_question, static_cast<cudaStream_t>(stream)) : PEVLM_OK;
+}
+
+// ---- sliding window: rows [first, first + n) of each sequence against its keys [0, first + n)
+static int check_window(const pevlm_shape_t* s, int32_t window, int64_t first, int64_t n) {
+    const int rc = check_shape(s);
+    if (rc != PEVLM_OK) return rc;
+    if (window < 1 || first < 0 || n < 0 || first > 1ll << 30 || n > 1ll << 30 || first + n > 1ll << 30) return PEVLM_EINVAL;
+    return PEVLM_OK;
+}
+
+// Few rows: 16-key pieces of sink and window, dealt to as many CTAs as there are.
+static QueryPlan plan_window(const pevlm_shape_t* s, int32_t window, int64_t first, int64_t n, DecodeParams* p) {
+    QueryPlan q{};
+    if (n * (s->num_q_heads / s->num_kv_heads) > kDecodeRows) return q;
+    const int pieces = static_cast<int>((first + n + 15) / 16);
+    const int64_t sink = s->sink_len < first + n ? s->sink_len : first + n;
+    const int sink_pieces = static_cast<int>((sink + 15) / 16);
+    const int64_t low = first - window + 1;  // first key in the first row's window
+    const int skip = low > 0 && low / 16 > sink_pieces ? static_cast<int>(low / 16) - sink_pieces : 0;
+    q.pieces = pieces - skip;
+    int64_t splits = kNumSms / (static_cast<int64_t>(s->num_kv_heads) * s->batch);
+    if (splits > (q.pieces + 7) / 8) splits = (q.pieces + 7) / 8;
+    if (splits < 1) splits = 1;
+    q.pieces_per_split = static_cast<int>((q.pieces + splits - 1) / splits);
+    q.n_splits = (q.pieces + q.pieces_per_split - 1) / q.pieces_per_split;
+    if (p) {
+        p->window = window < 1 << 30 ? window : 1 << 30;
+        p->sink = static_cast<int32_t>(sink);
+        p->sink_pieces = sink_pieces;
+        p->skip = skip;
+    }
+    return q;
+}
+
+size_t pevlm_window_workspace_bytes(const pevlm_shape_t* s, int32_t window, int64_t first_token, int64_t n_tokens) {
+    if (check_window(s, window, first_token, n_tokens) != PEVLM_OK) return 0;
+    // the most splits that any cache of such rows has: a step's workspace does for the next steps of its sequence
+    const int64_t rows = static_cast<int64_t>(s->batch) * n_tokens * s->num_q_heads;
+    if (n_tokens * (s->num_q_heads / s->num_kv_heads) > kDecodeRows) return kStatusBytes;
+    int64_t splits = kNumSms / (static_cast<int64_t>(s->num_kv_heads) * s->batch);
+    if (splits < 1) splits = 1;
+    return kStatusBytes + static_cast<size_t>(rows * splits) * (s->head_dim + 1) * sizeof(float);
+}
+
+int pevlm_window_attn(const pevlm_shape_t* s, int32_t window, const void* q, const void* k_cache, const void* v_cache, int64_t first_token,
+                      int64_t n_tokens, int64_t cache_rows, void* o, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_window(s, window, first_token, n_tokens);
+    if (rc != PEVLM_OK) return rc;
+    const int64_t keys = first_token + n_tokens;
+    if (cache_rows < keys || cache_rows > 1ll << 30) return PEVLM_EINVAL;
+    if (n_tokens > 0 && (!q || !k_cache || !v_cache || !o)) return PEVLM_EINVAL;
+    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned32(o) || !aligned16(lse)) return PEVLM_EALIGN;
+    if (!workspace || workspace_bytes < pevlm_window_workspace_bytes(s, window, first_token, n_tokens)) return PEVLM_EWORKSPACE;
+    if (!aligned256(workspace)) return PEVLM_EALIGN;
+    if (n_tokens == 0) return PEVLM_OK;
+    rc = check_device();
+    if (rc != PEVLM_OK) return rc;
+    const int d = s->head_dim;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    AttnParams p = common_params(s);
+    DecodeParams dp;
+    memset(&dp, 0, sizeof(dp));
+    const QueryPlan qp = plan_window(s, window, first_token, n_tokens, &dp);
+    p.hdr = static_cast<WorkspaceHeader*>(workspace);
+    if (qp.pieces > 0) {
+        p.Q = static_cast<int>(n_tokens);
+        p.n_splits = qp.n_splits;
+        dp.Q = p.Q; dp.L = static_cast<int>(keys); dp.n_video = static_cast<int>(first_token); dp.kv_rows = static_cast<int>(cache_rows);
+        dp.Hq = p.Hq; dp.Hkv = p.Hkv; dp.G = p.G;
+        dp.pieces = qp.pieces; dp.pieces_per_split = qp.pieces_per_split; dp.n_splits = qp.n_splits;
+        dp.scale = p.scale; dp.scale_log2 = p.scale_log2;
+        dp.hdr = p.hdr;
+        for (int b = 0; b < s->batch; b += 32768) {
+            p.batch = dp.batch = s->batch - b < 32768 ? s->batch - b : 32768;
+            p.part_o = dp.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kStatusBytes);
+            p.part_lse = dp.part_lse = p.part_o + static_cast<size_t>(p.batch) * p.n_splits * p.Q * p.Hq * d;
+            const int64_t q0 = b * n_tokens, k0 = b * cache_rows;
+            dp.q = rows_of(q, q0, p.Hq, d);
+            dp.k = rows_of(k_cache, k0, p.Hkv, d);
+            dp.v = rows_of(v_cache, k0, p.Hkv, d);
+            const cudaError_t e = launch_decode(dp, d, st);
+            if (e != cudaSuccess) return cuda_fail(e, "window decode launch");
+            rc = merge_question(p, d, const_cast<__nv_bfloat16*>(rows_of(o, q0, p.Hq, d)), lse ? lse + p.Hq * q0 : nullptr, st);
+            if (rc != PEVLM_OK) return rc;
+        }
+        return PEVLM_OK;
+    }
+    // the rows as the one segment of a full causal prefill of n_tokens, its items with the window's keys
+    pevlm_shape_t one = *s;
+    one.sink_len = 0; one.block_len = static_cast<int32_t>(n_tokens); one.num_blocks = 1; one.query_len = 0;
+    one.mask_mode = PEVLM_MASK_FULL_CAUSAL;
+    p = common_params(&one);
+    add_prefill(p, &one, false, 0, 0);
+    p.mode = 5;
+    p.div_items = make_divisor(p.n_items);
+    p.hdr = static_cast<WorkspaceHeader*>(workspace);
+    p.first_pos = static_cast<int>(first_token);
+    p.window = window < 1 << 30 ? window : 1 << 30;
+    p.sink_len = static_cast<int>(s->sink_len < keys ? s->sink_len : keys);
+    p.block_rows = static_cast<int>(keys);
+    p.blk_key0 = 0;
+    p.kv_rows = static_cast<int>(cache_rows);
+    const int step = launch_batch(s->batch, cache_rows > p.n_items ? cache_rows : p.n_items);
+    for (int b = 0; b < s->batch; b += step) {
+        p.batch = s->batch - b < step ? s->batch - b : step;
+        p.keep_status = b > 0;
+        const int64_t q0 = b * n_tokens, k0 = b * cache_rows;
+        AttnMaps m;
+        if ((rc = prefill_maps(m, p, d, rows_of(q, q0, p.Hq, d), rows_of(k_cache, k0, p.Hkv, d), rows_of(v_cache, k0, p.Hkv, d))) != PEVLM_OK) return rc;
+        p.o = const_cast<__nv_bfloat16*>(rows_of(o, q0, p.Hq, d));
+        p.lse = lse ? lse + p.Hq * q0 : nullptr;
+        const cudaError_t e = launch_attn(p, d, m, st);
+        if (e != cudaSuccess) return cuda_fail(e, "window attention launch");
+    }
+    return PEVLM_OK;
 }
 
 int pevlm_selftest_wait_expiry(void* workspace, size_t workspace_bytes, int64_t limit_ns, void* stream) {

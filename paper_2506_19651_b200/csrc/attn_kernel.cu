@@ -92,6 +92,7 @@ struct QSlot {
     int q_tok0, q_head0, row_div, ntok, nheads, qmap, box_rows;
     int per_div;  // ceil(2^16 / row_div): r / row_div = r * per_div >> 16 for r < 128
     int limit0;  // last visible key of row token 0, counted from the first key of the own range
+    int band_end0;  // sliding window: of row token 0, the end of the hidden keys (see WorkItem), counted in the same way
     int end;     // keys of the own range that the tile's rows can see at all
 };
 // Key tiles of an item: first the na tiles of the shared range [0, a_end) (the sink), then the tiles of the own
@@ -99,7 +100,9 @@ struct QSlot {
 // The own range is fetched at row b_coord0 of the block tensor map (own_map = 0), for the sink's own items of the sink map
 // (1), for question items of the map of the whole cache (2).  seq: sequence of the batch, a dimension of those maps of its own.
 // n_a, n_b: MMA columns of tile na - 1 and of the last tile; the others have 128.
+// Sliding window: keys of the own range from band on are hidden up to a row's band_end0 + token of the row.
 struct WorkItem {
+    int band;
     int kv_head, a_end, na, nt, n_a, n_b, split, b_coord0, own_map, seq;
     QSlot s[2];
 };
@@ -118,7 +121,8 @@ extern "C" int pevlm_debug_waits(unsigned* host_out) {
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ int cdiv(int a, int b) { return (a + b - 1) / b; }
 
-// MODE: bit 0 = the launch has prefill items, bit 1 = it has question items (handed out first: they are the longest).
+// MODE: bit 0 = the launch has prefill items, bit 1 = it has question items (handed out first: they are the longest), bit 2 (with bit 0
+// alone) = the prefill rows are one segment under a sliding window.
 // Items of a sequence follow one another, w counts over the whole batch.
 template <int MODE>
 __device__ __forceinline__ void decode_item(const AttnParams& p, int w, WorkItem& it) {
@@ -173,6 +177,24 @@ __device__ __forceinline__ void decode_item(const AttnParams& p, int w, WorkItem
             s.limit0 = tok;
             s.end = tok + s.ntok;
             if (s.valid) own_keys = max(own_keys, s.end);
+        }
+        if ((MODE & 4) && own_keys > 0) {
+            // The own range starts where the window of the pair's first row does, or at key 0 where that is within or right behind
+            // the sink: then it takes the sink in, whose keys the window does not hide.
+            const int low = it.s[1].valid ? min(it.s[0].limit0, it.s[1].limit0) : it.s[0].limit0;
+            const int start = p.first_pos + low - p.window + 1;
+            const bool apart = start > p.sink_len;
+            it.a_end = apart ? p.sink_len : 0;
+            it.b_coord0 = apart ? start : 0;
+            it.band = apart ? 0 : p.sink_len;
+            own_keys += p.first_pos - it.b_coord0;
+#pragma unroll 1
+            for (int x = 0; x < 2; ++x) {
+                QSlot& s = it.s[x];
+                s.limit0 += p.first_pos - it.b_coord0;
+                s.end += p.first_pos - it.b_coord0;
+                s.band_end0 = s.limit0 - p.window + 1;
+            }
         }
     } else {
         const int rest = quotient(w, p.div_splits);
@@ -635,6 +657,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
             // this row's last visible key and the smallest such key of the tile, counted from the own range's start
             const int end = uniform(qs.valid ? qs.end : 0), first_limit = uniform(qs.limit0);
             const int my_limit = min(first_limit + row_tok, end - 1), limit0 = min(first_limit, end - 1);
+            // sliding window: the row's hidden keys [band, my_band), and the most that a row of the tile has
+            const int band = uniform(it.band), my_band = qs.band_end0 + row_tok, last_band = uniform(qs.band_end0) + uniform(qs.ntok) - 1;
             __syncwarp();
             if (lane == 0) item_release(k);
             if (k == 0) grid_wait();
@@ -667,6 +691,19 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (i >= cols) r[c * 32 + i] = 0xff800000u;  // -inf
+                    }
+                }
+                if (MODE & 4) {
+                    const int key0 = (j - na) * kTile;
+                    if (j >= na && key0 < last_band && key0 + kTile > band) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const int from = band - key0 - c * 32, to = my_band - key0 - c * 32;  // hidden ones of this part
+                            if (__all_sync(0xffffffffu, to <= 0 || from >= 32)) continue;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (i >= from && i < to) r[c * 32 + i] = 0xff800000u;  // -inf
+                        }
                     }
                 }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -779,6 +816,7 @@ cudaError_t launch_attn(const AttnParams& p, int head_dim, const AttnMaps& m, cu
     // one cluster per work item; those that run take the rest from the hardware's queue
     const unsigned grid = 2u * static_cast<unsigned>(items);
 #define PEVLM_GO(D_, M_) launch_chained<attn_kernel<D_, M_>>(grid, kAttnThreads, smem, stream, p, m)
+    if (p.mode == 5) return head_dim == 128 ? PEVLM_GO(128, 5) : PEVLM_GO(64, 5);
     if (head_dim == 128) return p.mode == 1 ? PEVLM_GO(128, 1) : p.mode == 2 ? PEVLM_GO(128, 2) : PEVLM_GO(128, 3);
     return p.mode == 1 ? PEVLM_GO(64, 1) : p.mode == 2 ? PEVLM_GO(64, 2) : PEVLM_GO(64, 3);
 #undef PEVLM_GO

@@ -49,7 +49,8 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int D, int MT>
+// WINDOW: under a sliding window, see DecodeParams
+template <int D, int MT, bool WINDOW>
 __global__ void __launch_bounds__(kDecodeThreads, 1) decode_kernel(const __grid_constant__ DecodeParams p) {
     using L = DecodeSmem<D, MT>;
     constexpr int ROWS = L::kRows;
@@ -64,12 +65,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) decode_kernel(const __grid_
     const int pieces = min(p.pieces_per_split, p.pieces - piece0);
     const int mine = pieces > warp ? (pieces - warp + kDecodeWarps - 1) / kDecodeWarps : 0;  // pieces of this warp
     const int64_t row_stride = static_cast<int64_t>(p.Hkv) * D;
-    const __nv_bfloat16* k = p.k + seq * p.L * row_stride + g * D;
-    const __nv_bfloat16* v = p.v + seq * p.L * row_stride + g * D;
+    const __nv_bfloat16* k = p.k + seq * p.kv_rows * row_stride + g * D;
+    const __nv_bfloat16* v = p.v + seq * p.kv_rows * row_stride + g * D;
+    auto key_of = [&](int piece) { return (WINDOW && piece >= p.sink_pieces ? piece + p.skip : piece) * kPiece; };
     // While the kernels before this one finish (a decode step's RoPE and copy of one token leave nearly all SMs idle), the
     // first pieces are brought into L2: that reads nothing, so what those kernels still write is seen all the same.
     for (int n = 0; n < min(mine, kEarlyPieces); ++n) {
-        const int key0 = (piece0 + warp + n * kDecodeWarps) * kPiece;
+        const int key0 = key_of(piece0 + warp + n * kDecodeWarps);
         constexpr int kLines = D * 2 / 128;  // lines of a row
         for (int i = lane; i < kPiece * kLines; i += 32) {
             const int64_t key = min(key0 + i / kLines, p.L - 1);
@@ -84,7 +86,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) decode_kernel(const __grid_
 
     auto fetch = [&](int n) {  // the warp's n-th piece
         if (n < mine) {
-            const int key0 = (piece0 + warp + n * kDecodeWarps) * kPiece;
+            const int key0 = key_of(piece0 + warp + n * kDecodeWarps);
             const uint32_t stage = ring + (n % L::kStages) * L::kStageBytes;
 #pragma unroll
             for (int i = 0; i < kPiece * CH / 32; ++i) {
@@ -132,7 +134,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) decode_kernel(const __grid_
         asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 1) : "memory");
         __syncwarp();
         const uint32_t stage = ring + (n % L::kStages) * L::kStageBytes;
-        const int key0 = (piece0 + warp + n * kDecodeWarps) * kPiece;
+        const int key0 = key_of(piece0 + warp + n * kDecodeWarps);
         float s[MT][2][4] = {};  // keys [0, 8) and [8, 16)
         const int krow = (mat >> 1) * 8 + mrow, vrow = (mat & 1) * 8 + mrow;
 #pragma unroll
@@ -156,6 +158,15 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) decode_kernel(const __grid_
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (key0 + i * 8 + (lane & 3) * 2 + (e & 1) > limit[t][e >> 1]) s[t][i][e] = -INFINITY;
+            }
+            if (WINDOW && key0 <= p.L - 1 - p.window && key0 + kPiece > p.sink) {  // the last row's window begins behind some of these
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = key0 + i * 8 + (lane & 3) * 2 + (e & 1);
+                        if (key <= limit[t][e >> 1] - p.window && key >= p.sink) s[t][i][e] = -INFINITY;
+                    }
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -240,14 +251,19 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) decode_kernel(const __grid_
     }
 }
 
-cudaError_t launch_decode(const DecodeParams& p, int head_dim, cudaStream_t stream) {
+template <bool WINDOW>
+static cudaError_t launch_form(const DecodeParams& p, int head_dim, cudaStream_t stream) {
     const dim3 grid(static_cast<unsigned>(p.n_splits), static_cast<unsigned>(p.Hkv), static_cast<unsigned>(p.batch));
     const bool two = p.Q * p.G > 16;
     if (head_dim == 128)
-        return two ? launch_chained<decode_kernel<128, 2>>(grid, kDecodeThreads, DecodeSmem<128, 2>::kTotal, stream, p)
-                   : launch_chained<decode_kernel<128, 1>>(grid, kDecodeThreads, DecodeSmem<128, 1>::kTotal, stream, p);
-    return two ? launch_chained<decode_kernel<64, 2>>(grid, kDecodeThreads, DecodeSmem<64, 2>::kTotal, stream, p)
-               : launch_chained<decode_kernel<64, 1>>(grid, kDecodeThreads, DecodeSmem<64, 1>::kTotal, stream, p);
+        return two ? launch_chained<decode_kernel<128, 2, WINDOW>>(grid, kDecodeThreads, DecodeSmem<128, 2>::kTotal, stream, p)
+                   : launch_chained<decode_kernel<128, 1, WINDOW>>(grid, kDecodeThreads, DecodeSmem<128, 1>::kTotal, stream, p);
+    return two ? launch_chained<decode_kernel<64, 2, WINDOW>>(grid, kDecodeThreads, DecodeSmem<64, 2>::kTotal, stream, p)
+               : launch_chained<decode_kernel<64, 1, WINDOW>>(grid, kDecodeThreads, DecodeSmem<64, 1>::kTotal, stream, p);
+}
+
+cudaError_t launch_decode(const DecodeParams& p, int head_dim, cudaStream_t stream) {
+    return p.window > 0 ? launch_form<true>(p, head_dim, stream) : launch_form<false>(p, head_dim, stream);
 }
 
 }  // namespace pevlm

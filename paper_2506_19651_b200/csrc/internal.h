@@ -104,7 +104,7 @@ struct Segment {
 };
 
 // What one launch of the attention kernel does, bit 0 of mode: prefill rows (sink + blocks, or full causal); bit 1:
-// question rows against the assembled cache, split over keys.
+// question rows against the assembled cache, split over keys; bit 2 (with bit 0): rows under a sliding window, seg[0] alone.
 struct AttnParams {
     int32_t mode;
     int32_t batch;          // sequences, each with n_items work items
@@ -136,6 +136,8 @@ struct AttnParams {
     WorkspaceHeader* hdr;
     WorkspaceHeader* hdr_question;  // mode 3: header of the question's workspace
     int32_t keep_status;    // a later launch of the same call
+    int32_t first_pos;      // sliding window: position of the first row,
+    int32_t window;         // and positions that a row sees, its own among them (beside the first sink_len)
 };
 
 constexpr int kMergeRows = 8 * kNumSms;  // most rows of the merge that takes a CTA for each (as many as are resident)
@@ -150,10 +152,14 @@ struct DecodeParams {
     float* part_lse;         // [batch, n_splits, Q, Hq]
     WorkspaceHeader* hdr;
     int32_t batch, Q, L, n_video, Hq, Hkv, G;
-    int32_t pieces;            // ceil(L / 16)
+    int32_t kv_rows;           // rows from one sequence to the next
+    int32_t pieces;            // ceil(L / 16), without the skipped ones
     int32_t pieces_per_split;
     int32_t n_splits;
     float scale, scale_log2;
+    // sliding window (0: none) beside the first `sink` keys; pieces from sink_pieces on are `skip` further on, where nothing between
+    // the sink and the window of the first row is visible
+    int32_t window, sink, sink_pieces, skip;
 };
 
 struct MergeParams {

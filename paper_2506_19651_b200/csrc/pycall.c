@@ -94,6 +94,11 @@ BEGIN(layer_forward, 18)
     int64_t wqb = I(16); void* st = P(17);
 END(pevlm_layer_forward(s, (int32_t)last, q, k, v, qv, qq, kc, vc, ov, (float*)lv, oq, (float*)lq, wp, (size_t)wpb, wq, (size_t)wqb, st))
 
+BEGIN(window_attn, 13)
+    int64_t window = I(1); void *q = P(2), *k = P(3), *v = P(4); int64_t first = I(5), tokens = I(6), rows = I(7);
+    void *o = P(8), *lse = P(9), *ws = P(10); int64_t wb = I(11); void* st = P(12);
+END(pevlm_window_attn(s, (int32_t)window, q, k, v, first, tokens, rows, o, (float*)lse, ws, (size_t)wb, st))
+
 /* The calls on pages: the first argument is the address of a pevlm_pages_t, or of a shape with the pages behind it. */
 BEGIN(pages_release, 9)
     void *fin = P(1), *len = P(2), *tab = P(3), *fl = P(4), *fc = P(5), *lo = P(6), *fo = P(7), *st = P(8);
@@ -121,7 +126,8 @@ END(pevlm_packed_attn(s, (const pevlm_pages_t*)g, (int32_t)window, q, qs, c, tab
 static PyMethodDef methods[] = {METHOD(rope_qk), METHOD(rope_qkv), METHOD(rope_qk_mrope), METHOD(parallel_prefill_attn),
                                 METHOD(block_attn), METHOD(assemble_kv), METHOD(query_attn), METHOD(query_attn_noalloc),
                                 METHOD(layer_forward), METHOD(pages_release), METHOD(pages_assign),
-                                METHOD(packed_store), METHOD(packed_load), METHOD(packed_attn), {NULL, NULL, 0, NULL}};
+                                METHOD(packed_store), METHOD(packed_load), METHOD(packed_attn),
+                                METHOD(window_attn), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pevlm_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__pevlm_call(void) {

@@ -143,3 +143,26 @@ def test_reference_allocator():
     assert slots[:18].tolist() == list(range(80, 96)) + [64, 48] and (slots[18:] == -1).all() and start.tolist() == [0, 17, 18, 78]
     lens, free, count = a.release([0, 1, 0], lens, table, free, count)
     assert lens.tolist() == [17, 0, 0] and count == 4 and free[3] == 3
+
+
+def test_window_attn(lib):
+    s, p = pb.make_shape(4, 1, 0, 1, 4, 2, 64), at(4096)
+    size = pb.pevlm_window_workspace_bytes(s, 100, 50, 4)
+    names = dict(window=100, q=p, k=p, v=p, first=50, n=4, rows=54, o=p, lse=p, ws=p, wb=size)
+    attn = lambda s=s, **kw: lib.pevlm_window_attn(C.byref(s), *(dict(names, **kw)[n] for n in names), None)
+    for field, val, code in (("head_dim", 96, pb.PEVLM_EUNSUPPORTED), ("num_kv_heads", 3, pb.PEVLM_EINVAL), ("batch", 0, pb.PEVLM_EINVAL),
+                             ("softmax_scale", -1.0, pb.PEVLM_EINVAL), ("sink_len", -1, pb.PEVLM_EINVAL)):
+        bad = pb.make_shape(4, 1, 0, 1, 4, 2, 64)
+        setattr(bad, field, val)
+        assert attn(s=bad) == code and pb.pevlm_window_workspace_bytes(bad, 100, 50, 4) == 0, field
+    for name in ("q", "k", "v", "o"):
+        assert attn(**{name: None}) == pb.PEVLM_EINVAL and attn(**{name: at(4098)}) == pb.PEVLM_EALIGN, name
+    assert attn(lse=at(4100)) == pb.PEVLM_EALIGN and attn(o=at(4096 + 16)) == pb.PEVLM_EALIGN
+    for window, first, n in ((0, 50, 4), (-1, 50, 4), (100, -1, 4), (100, 50, -1), (100, 2 ** 30, 1), (100, 2 ** 62, 2 ** 62)):
+        assert attn(window=window, first=first, n=n, rows=2 ** 30) == pb.PEVLM_EINVAL
+        assert pb.pevlm_window_workspace_bytes(s, window, first, n) == 0
+    assert attn(rows=53) == pb.PEVLM_EINVAL and attn(rows=2 ** 30 + 1) == pb.PEVLM_EINVAL
+    assert attn(ws=None) == pb.PEVLM_EWORKSPACE and attn(wb=size - 1) == pb.PEVLM_EWORKSPACE and attn(ws=at(4096 + 128)) == pb.PEVLM_EALIGN
+    assert attn(n=0, q=None, k=None, v=None, o=None) == pb.PEVLM_OK
+    # one workspace for any cache and window of the same rows
+    assert pb.pevlm_window_workspace_bytes(s, 1, 0, 4) == size == pb.pevlm_window_workspace_bytes(s, 2 ** 31 - 1, 10 ** 6, 4)
