@@ -234,12 +234,18 @@ cudaError_t launch_packed_store(const PackedRows& p, int head_dim, cudaStream_t 
 cudaError_t launch_packed_load(const PackedRows& p, int head_dim, cudaStream_t stream);
 
 // Attention over the packed cache (packed_attn_kernel.cu).
+struct __align__(16) PackedJoin {  // what CTA c of the launch leaves unfinished and is the first of
+    int32_t last;      // last CTA with a share of it; nothing to join where that is not behind c
+    int32_t second;    // c's own share stands in its second place
+    int32_t row0, n, head, chunk;
+};
 struct PackedAttnParams {
     const __nv_bfloat16* q;  // rows q_stride elements apart
     const uint8_t* cache;
     const int32_t *page_table, *lens, *row_start;
     __nv_bfloat16* o;        // [n_rows, Hq, d]
     float* lse;              // [Hq, n_rows] or NULL
+    PackedJoin* joins;       // one for each CTA
     float* part;             // shares of units that cross from one CTA into the next, two places for each CTA
     int64_t q_stride;
     int32_t n_rows, num_seqs, num_pages, max_pages, page_shift;

@@ -157,7 +157,8 @@ int pevlm_packed_attn(const pevlm_shape_t* s, const pevlm_pages_t* g, int32_t wi
     p.page_table = page_table; p.lens = lens; p.row_start = row_start;
     p.o = static_cast<__nv_bfloat16*>(o);
     p.lse = lse;
-    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kStatusBytes);
+    p.joins = reinterpret_cast<PackedJoin*>(static_cast<uint8_t*>(workspace) + kStatusBytes);
+    p.part = reinterpret_cast<float*>(p.joins + kNumSms);
     p.q_stride = q_stride;
     p.n_rows = static_cast<int32_t>(n_rows);
     p.num_seqs = g->num_seqs; p.num_pages = g->num_pages; p.max_pages = g->max_pages; p.page_shift = page_shift(g);

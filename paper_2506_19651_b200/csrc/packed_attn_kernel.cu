@@ -26,17 +26,19 @@
 
 namespace pevlm {
 
+constexpr uint32_t kNoTile = 0xffffffffu;
 constexpr float kNoMax = -3.0e38f;  // running maximum of a row that has seen no key: any score raises it
 
 template <int D, int NT>
 struct PackedAttnLayout {
     static constexpr int kWarps = NT == 1 ? 12 : 8;
-    static constexpr int kStages = D == 128 ? 4 : 8;
-    static constexpr int kTileBytes = 18 * D;
+    static constexpr int kStages = D == 128 ? 3 + (NT == 2) : 6;  // steps (two tiles) in a warp's ring
+    static constexpr int kTileBytes = 18 * D, kStepBytes = 2 * kTileBytes;
     static constexpr int kRows = 8 * NT;
     static constexpr int kShareFloats = kRows * (D + 2);          // O [rows][D], then m and l of each row
-    static constexpr int kRing = kWarps * kStages * kTileBytes;
-    static constexpr int kTotal = kRing + kWarps * 2 * kShareFloats * 4;
+    static constexpr int kRing = kWarps * kStages * kStepBytes;
+    static constexpr int kTotal = kRing + kWarps * kShareFloats * 4;
+    static_assert(kShareFloats * 4 <= kStages * kStepBytes, "the second share of a warp is left in its ring");
 };
 
 // One sequence of the call as the tiles see it.
@@ -69,34 +71,95 @@ __device__ __forceinline__ int64_t part_start(int64_t w, int64_t total, int n_wo
 __device__ __forceinline__ int worker_of(int64_t tile, int64_t total, int n_workers) { return static_cast<int>(((tile + 1) * n_workers - 1) / total); }
 __device__ __forceinline__ int workers_for(int64_t total, int most) { return static_cast<int>(min(static_cast<int64_t>(most), (total + 1) / 2)); }
 
-// By a whole warp: tiles of all sequences; with `tile` >= 0 also the sequence that it belongs to and the tiles before that sequence.
-__device__ __forceinline__ int64_t find_seq(const PackedAttnParams& p, int rows_per_chunk, int64_t tile, int& seq, int64_t& before) {
-    const int lane = threadIdx.x & 31;
-    int64_t base = 0;
-    for (int r0 = 0; r0 < p.num_seqs; r0 += 32) {
-        int64_t mine = 0;
-        if (r0 + lane < p.num_seqs) {
-            const PackedSeq s = packed_seq(p, r0 + lane, rows_per_chunk);
-            mine = static_cast<int64_t>(s.chunks) * s.cnt * p.Hkv;
-        }
-        int64_t to = mine;
+__device__ __forceinline__ int64_t seq_tiles(const PackedAttnParams& p, int r, int rows_per_chunk) {
+    if (r >= p.num_seqs) return 0;
+    const PackedSeq s = packed_seq(p, r, rows_per_chunk);
+    return static_cast<int64_t>(s.chunks) * s.cnt * p.Hkv;
+}
+
+__device__ __forceinline__ int64_t warp_inclusive(int64_t x) {
 #pragma unroll
-        for (int by = 1; by < 32; by *= 2) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, to, by);
-            if (lane >= by) to += y;
+    for (int by = 1; by < 32; by *= 2) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, by);
+        if ((threadIdx.x & 31) >= static_cast<unsigned>(by)) x += y;
+    }
+    return x;
+}
+
+// The calling warp's part of the list: tiles [lo, hi) of `total`, beginning `off` tiles into those of sequence seq.
+struct PackedPart {
+    int64_t total, lo, hi, off;
+    int seq, n_workers;
+};
+
+template <int W>
+__device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int rows_per_chunk) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, me = blockIdx.x * W + warp;
+    PackedPart part;
+    part.seq = 0;
+    part.off = 0;
+    auto bounds = [&](int64_t total) {
+        part.total = total;
+        part.n_workers = workers_for(total, gridDim.x * W);
+        part.lo = me < part.n_workers ? part_start(me, total, part.n_workers) : total;
+        part.hi = me < part.n_workers ? part_start(me + 1, total, part.n_workers) : total;
+    };
+    if (p.num_seqs <= 32) {  // each warp for itself
+        const int64_t mine = seq_tiles(p, lane, rows_per_chunk), to = warp_inclusive(mine);
+        bounds(__shfl_sync(0xffffffffu, to, 31));
+        const unsigned past = __ballot_sync(0xffffffffu, to > part.lo);
+        if (past) {
+            part.seq = __ffs(past) - 1;
+            part.off = part.lo - __shfl_sync(0xffffffffu, to - mine, part.seq);
         }
-        if (tile >= 0) {
-            const unsigned past = __ballot_sync(0xffffffffu, base + to > tile);
-            if (past) {
-                const int l = __ffs(past) - 1;
-                seq = r0 + l;
-                before = base + __shfl_sync(0xffffffffu, to - mine, l);
-                return 0;
+        return part;
+    }
+    // a thread for every sequence, W * 32 at a time
+    __shared__ int64_t s_sum[W], s_off[W];
+    __shared__ int s_seq[W];
+    int64_t sum = 0;
+    for (int r = threadIdx.x; r < p.num_seqs; r += W * 32) sum += seq_tiles(p, r, rows_per_chunk);
+    sum = warp_inclusive(sum);
+    if (lane == 31) s_sum[warp] = sum;
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) total += s_sum[w];
+    bounds(total);
+    int64_t base = 0;
+    for (int r0 = 0; r0 < p.num_seqs; r0 += W * 32) {
+        const int r = r0 + threadIdx.x;
+        const int64_t mine = seq_tiles(p, r, rows_per_chunk);
+        int64_t to = warp_inclusive(mine);
+        __syncthreads();
+        if (lane == 31) s_sum[warp] = to;
+        __syncthreads();
+        int64_t all = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (w < warp) to += s_sum[w];
+            all += s_sum[w];
+        }
+        to += base;
+        if (mine > 0) {
+            for (int w = 0; w < W; ++w) {
+                const int worker = blockIdx.x * W + w;
+                if (worker >= part.n_workers) break;
+                const int64_t lo = part_start(worker, total, part.n_workers);
+                if (lo >= to - mine && lo < to) {
+                    s_seq[w] = r;
+                    s_off[w] = lo - (to - mine);
+                }
             }
         }
-        base += __shfl_sync(0xffffffffu, to, 31);
+        base += all;
     }
-    return base;
+    __syncthreads();
+    if (part.hi > part.lo) {
+        part.seq = s_seq[warp];
+        part.off = s_off[warp];
+    }
+    return part;
 }
 
 // A place on the list.
@@ -122,13 +185,14 @@ struct PackedCursor {
             s = packed_seq(p, r, rows_per_chunk);
         } while (s.chunks == 0);
     }
-    __device__ __forceinline__ int key_tile() const { return t < s.ns ? t : t + s.skip; }
-    // Page of the tile, -1 where there is nothing to read.
-    __device__ __forceinline__ int page(const PackedAttnParams& p) const {
-        const int key0 = key_tile() << 4;
-        if (key0 >= s.len) return -1;
-        const int pg = __ldcg(p.page_table + static_cast<int64_t>(r) * p.max_pages + (key0 >> p.page_shift));
-        return pg >= 0 && pg < p.num_pages ? pg : -1;
+    __device__ __forceinline__ int key0(int x) const { return (x < s.ns ? x : x + s.skip) << 4; }
+    // Where tile x of the unit stands in the cache, in units of 128 bytes (which tile_units of them make); kNoTile where there is nothing to read.
+    __device__ __forceinline__ uint32_t place(const PackedAttnParams& p, int x, int tile_units) const {
+        const int tile = x < s.ns ? x : x + s.skip;
+        if (x >= s.cnt || tile << 4 >= s.len) return kNoTile;
+        const int page = __ldcg(p.page_table + static_cast<int64_t>(r) * p.max_pages + (tile >> (p.page_shift - 4)));
+        if (page < 0 || page >= p.num_pages) return kNoTile;
+        return static_cast<uint32_t>((((static_cast<int64_t>(page) * p.Hkv + head) << (p.page_shift - 4)) + (tile & ((1 << (p.page_shift - 4)) - 1))) * tile_units);
     }
 };
 
@@ -179,60 +243,78 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
     using L = PackedAttnLayout<D, NT>;
     constexpr int W = L::kWarps, KS = D / 16, MT = D / 16;  // k-steps of S, row tiles of V^T
     constexpr int kWords = D / 32;                          // words of codes: of a key in a thread of S; twice what an eighth of the head has
+    constexpr int kChunks = L::kTileBytes / 16;             // of 16 bytes
     extern __shared__ __align__(128) uint8_t raw[];
     struct Share {       // a share left for the CTA to join
         int64_t u0, u1;  // tiles of its unit, counted over the whole list
         int r, head, chunk, row0, n;
-        int from_start;  // the part of the warp begins with it
     };
     __shared__ Share s_share[2 * W];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const uint32_t ring = smem_u32(raw) + warp * L::kStages * L::kTileBytes;
-    float* const shares = reinterpret_cast<float*>(raw + L::kRing);
+    uint8_t* const my_ring = raw + warp * L::kStages * L::kStepBytes;
+    const uint32_t ring = smem_u32(my_ring);
+    // a warp's first share has a place of its own, the second, with which its part ends, takes the ring
+    auto share_at = [&](int slot) { return reinterpret_cast<float*>(slot & 1 ? raw + (slot >> 1) * L::kStages * L::kStepBytes : raw + L::kRing + (slot >> 1) * L::kShareFloats * 4); };
     if (lane < 2) s_share[2 * warp + lane].u1 = -1;
+    __syncwarp();
     grid_wait();
 
-    int seq = 0;
-    int64_t before = 0;
-    const int64_t total = find_seq(p, L::kRows, -1, seq, before);
-    const int n_workers = workers_for(total, gridDim.x * W);
-    const int me = blockIdx.x * W + warp;
-    const int64_t lo = me < n_workers ? part_start(me, total, n_workers) : total;
-    const int64_t hi = me < n_workers ? part_start(me + 1, total, n_workers) : total;
-    const int mine = static_cast<int>(hi - lo);
+    const PackedPart part = my_part<W>(p, L::kRows);
+    const int mine = static_cast<int>(part.hi - part.lo);
     grid_launch_dependents();
     if (mine > 0) {
-        find_seq(p, L::kRows, lo, seq, before);
         PackedCursor cur, ahead;
-        cur.at(p, L::kRows, seq, lo - before);
+        cur.at(p, L::kRows, part.seq, part.off);
         ahead = cur;
-        int next_page = ahead.page(p);
-        unsigned there = 0;  // of the ring's places: the tile exists
-        const int tiles_per_page = 1 << (p.page_shift - 4);
-        auto fetch = [&](int i) {
-            if (i < mine) {
-                const int place = i % L::kStages;
-                there &= ~(1u << place);
-                if (next_page >= 0) {
-                    there |= 1u << place;
-                    const uint8_t* src = p.cache + ((static_cast<int64_t>(next_page) * p.Hkv + ahead.head) * tiles_per_page + (ahead.key_tile() & (tiles_per_page - 1))) * L::kTileBytes;
-                    const uint32_t dst = ring + place * L::kTileBytes;
-#pragma unroll
-                    for (int c = lane; c < L::kTileBytes / 16; c += 32)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c * 16), "l"(src + c * 16) : "memory");
+        // Fetching: steps of two tiles.  A lane holds the place of a tile, 32 tiles at a time and the 32 behind them, so that a page
+        // is looked up long before it is needed.
+        int to_fetch = mine, left = min(ahead.s.cnt - ahead.t, to_fetch);  // of the part, and of it in this unit
+        int block = ahead.t;
+        uint32_t places = ahead.place(p, block + lane, L::kTileBytes / 128), places_next = ahead.place(p, block + 32 + lane, L::kTileBytes / 128);
+        unsigned there = 0;  // two bits a place in the ring: the tiles exist
+        int stage_in = 0;
+        auto fetch = [&]() {
+            if (to_fetch > 0) {
+                if (ahead.t - block == 32) {
+                    block += 32;
+                    places = places_next;
+                    places_next = ahead.place(p, block + 32 + lane, L::kTileBytes / 128);
                 }
-                if (++ahead.t == ahead.s.cnt) ahead.next_unit(p, L::kRows);
-                if (i + 1 < mine) next_page = ahead.page(p);
+                const uint32_t at0 = __shfl_sync(0xffffffffu, places, ahead.t - block), at1 = left > 1 ? __shfl_sync(0xffffffffu, places, ahead.t - block + 1) : kNoTile;
+                there = (there & ~(3u << (2 * stage_in))) | ((at0 != kNoTile ? 1u : 0u) | (at1 != kNoTile ? 2u : 0u)) << (2 * stage_in);
+                const uint8_t* const src0 = p.cache + static_cast<uint64_t>(at0) * 128 + lane * 16;
+                const uint8_t* const src1 = p.cache + static_cast<uint64_t>(at1) * 128 + lane * 16 - kChunks % 32 * 16;
+                const uint32_t dst = ring + stage_in * L::kStepBytes + lane * 16;
+                // the chunks of both tiles, 32 at a time: those in the middle are of one or the other (kChunks % 32 = 16 or 8)
+#pragma unroll
+                for (int c = 0; c < (2 * kChunks + 31) / 32; ++c) {
+                    const bool first = c * 32 + lane < kChunks;
+                    const uint8_t* const src = first ? src0 + c * 512 : src1 + (c - kChunks / 32) * 512;
+                    const bool some = (first ? at0 : at1) != kNoTile && ((c + 1) * 32 <= 2 * kChunks || c * 32 + lane < 2 * kChunks);
+                    if (some) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c * 512), "l"(src) : "memory");
+                }
+                stage_in = stage_in + 1 == L::kStages ? 0 : stage_in + 1;
+                const int step = min(left, 2);
+                to_fetch -= step;
+                left -= step;
+                ahead.t += step;
+                if (left == 0 && to_fetch > 0) {
+                    ahead.next_unit(p, L::kRows);
+                    left = min(ahead.s.cnt, to_fetch);
+                    block = 0;
+                    places = ahead.place(p, lane, L::kTileBytes / 128);
+                    places_next = ahead.place(p, 32 + lane, L::kTileBytes / 128);
+                }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        for (int i = 0; i < L::kStages - 1; ++i) fetch(i);
+        for (int i = 0; i < L::kStages - 1; ++i) fetch();
 
-        int64_t unit0 = lo - cur.t;  // of this unit on the list
-        int i = 0;
-        while (i < mine) {
+        int64_t unit0 = part.lo - cur.t;  // of this unit on the list
+        int stage = 0, done_tiles = 0;
+        while (done_tiles < mine) {
             // ------------------------------------------------ a unit, or the share of it that is in this part
-            const int first_tile = cur.t, tiles = min(cur.s.cnt - cur.t, mine - i);
+            const int first_tile = cur.t, tiles = min(cur.s.cnt - cur.t, mine - done_tiles);
             const int rows = min(cur.s.n * p.G - cur.chunk * L::kRows, L::kRows);
             uint32_t q[NT][KS][2];
             float sc[NT][2];                // softmax scale, in units of log2, of rows 2 t and 2 t + 1
@@ -277,83 +359,96 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
             pos_min = cur.s.len - cur.s.n + quotient(cur.chunk * L::kRows, p.div_g);
             pos_max = cur.s.len - cur.s.n + quotient(cur.chunk * L::kRows + rows - 1, p.div_g);
 
-            for (int n = 0; n < tiles; ++n, ++i) {
-                fetch(i + L::kStages - 1);
+            for (int n = 0; n < tiles; n += 2) {
+                fetch();
                 asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 1) : "memory");
                 __syncwarp();
-                const int place = i % L::kStages;
-                const int key0 = cur.key_tile() << 4;
-                ++cur.t;
-                if (!(there >> place & 1)) continue;
-                const uint8_t* const tile = raw + (warp * L::kStages + place) * L::kTileBytes;
-                // S^T: keys g and g + 8, rows 2 t and 2 t + 1
-                float s[NT][4];
+                const uint8_t* const step = my_ring + stage * L::kStepBytes;
+                const unsigned exist = there >> (2 * stage) & 3u;
+                stage = stage + 1 == L::kStages ? 0 : stage + 1;
+                const int key0[2] = {cur.key0(first_tile + n), cur.key0(first_tile + n + 1)};
+                if (exist == 0) continue;
+                // S^T: keys g and g + 8 of either tile, rows 2 t and 2 t + 1
+                float s[NT][2][4];
+                uint32_t vs[2][2];  // V's scales of keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
 #pragma unroll
-                for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-                uint32_t kw[2][kWords], ks[2][2];  // codes and scales (twice in a word) of keys g and g + 8
-                if (D == 128) {
+                for (int x = 0; x < 2; ++x) {
+                    const uint8_t* const tile = step + x * L::kTileBytes;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(&kw[h][0]) = *reinterpret_cast<const uint4*>(tile + h * 512 + lane * 16);
-                    const uint32_t sb = *reinterpret_cast<const uint32_t*>(tile + 16 * D + lane * 4);
+                    for (int j = 0; j < NT; ++j) s[j][x][0] = s[j][x][1] = s[j][x][2] = s[j][x][3] = 0.f;
+                    uint32_t kw[2][kWords], ks[2][2];  // codes and scales (twice in a word) of keys g and g + 8
+                    if (D == 128) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t two = scale_pair(sb >> (16 * h));
-                        ks[h][0] = __byte_perm(two, 0, 0x1010);
-                        ks[h][1] = __byte_perm(two, 0, 0x3232);
-                    }
-                } else {
+                        for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(&kw[h][0]) = *reinterpret_cast<const uint4*>(tile + h * 512 + lane * 16);
+                        const uint32_t sb = *reinterpret_cast<const uint32_t*>(tile + 16 * D + lane * 4);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) *reinterpret_cast<uint2*>(&kw[h][0]) = *reinterpret_cast<const uint2*>(tile + h * 256 + lane * 8);
-                    const uint32_t two = scale_pair(*reinterpret_cast<const uint16_t*>(tile + 16 * D + lane * 2));
-                    ks[0][0] = ks[0][1] = __byte_perm(two, 0, 0x1010);
-                    ks[1][0] = ks[1][1] = __byte_perm(two, 0, 0x3232);
-                }
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t two = scale_pair(sb >> (16 * h));
+                            ks[h][0] = __byte_perm(two, 0, 0x1010);
+                            ks[h][1] = __byte_perm(two, 0, 0x3232);
+                        }
+                    } else {
 #pragma unroll
-                for (int w = 0; w < kWords; ++w) {
-                    uint32_t a[2][4];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        halves_of_word(kw[h][w], a[h]);
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) a[h][b] = mul_f16x2(a[h][b], ks[h][w >> 1]);
+                        for (int h = 0; h < 2; ++h) *reinterpret_cast<uint2*>(&kw[h][0]) = *reinterpret_cast<const uint2*>(tile + h * 256 + lane * 8);
+                        const uint32_t two = scale_pair(*reinterpret_cast<const uint16_t*>(tile + 16 * D + lane * 2));
+                        ks[0][0] = ks[0][1] = __byte_perm(two, 0, 0x1010);
+                        ks[1][0] = ks[1][1] = __byte_perm(two, 0, 0x3232);
                     }
 #pragma unroll
-                    for (int half = 0; half < 2; ++half)
+                    for (int w = 0; w < kWords; ++w) {
+                        uint32_t a[2][4];
 #pragma unroll
-                        for (int j = 0; j < NT; ++j)
-                            mma16816_f16(s[j], a[0][2 * half], a[1][2 * half], a[0][2 * half + 1], a[1][2 * half + 1], q[j][2 * w + half][0], q[j][2 * w + half][1]);
-                }
-                // V's scales of keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9; of keys behind the end, whose bytes may be anything, 0
-                uint32_t vs[2];
-                const uint32_t vb = *reinterpret_cast<const uint32_t*>(tile + 17 * D + (D == 128 ? lane * 4 : (g >> 1) * 16 + t * 4));
-                vs[0] = scale_pair(vb);
-                vs[1] = scale_pair(vb >> 16);
-                const bool edge = key0 + 15 > pos_min || (p.window > 0 && key0 <= pos_max - p.window && key0 + 15 >= p.sink);
-                if (edge) {
+                        for (int h = 0; h < 2; ++h) {
+                            halves_of_word(kw[h][w], a[h]);
 #pragma unroll
-                    for (int j = 0; j < NT; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int key = key0 + g + (e >> 1) * 8, at = pos[j][e & 1];
-                            if (key > at || (p.window > 0 && key <= at - p.window && key >= p.sink)) s[j][e] = -INFINITY;
+                            for (int b = 0; b < 4; ++b) a[h][b] = mul_f16x2(a[h][b], ks[h][w >> 1]);
                         }
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (key0 + 8 * h + 2 * t >= cur.s.len) vs[h] = 0u;
-                        else if (key0 + 8 * h + 2 * t + 1 >= cur.s.len) vs[h] &= 0xffffu;
+                        for (int half = 0; half < 2; ++half)
+#pragma unroll
+                            for (int j = 0; j < NT; ++j)
+                                mma16816_f16(s[j][x], a[0][2 * half], a[1][2 * half], a[0][2 * half + 1], a[1][2 * half + 1], q[j][2 * w + half][0], q[j][2 * w + half][1]);
+                    }
+                    const uint32_t vb = *reinterpret_cast<const uint32_t*>(tile + 17 * D + (D == 128 ? lane * 4 : (g >> 1) * 16 + t * 4));
+                    vs[x][0] = scale_pair(vb);
+                    vs[x][1] = scale_pair(vb >> 16);
+                }
+                // masks, and scales of 0 for what is behind the end or not there (its bytes may be anything)
+                const int last0 = max(key0[0], key0[1]);
+                if (exist != 3u || last0 + 15 > pos_min || (p.window > 0 && key0[0] <= pos_max - p.window && last0 + 15 >= p.sink)) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const bool is_there = exist >> x & 1;
+#pragma unroll
+                        for (int j = 0; j < NT; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int key = key0[x] + g + (e >> 1) * 8, at = pos[j][e & 1];
+                                if (!is_there || key > at || (p.window > 0 && key <= at - p.window && key >= p.sink)) s[j][x][e] = -INFINITY;
+                            }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (!is_there || key0[x] + 8 * h + 2 * t >= cur.s.len) vs[x][h] = 0u;
+                            else if (key0[x] + 8 * h + 2 * t + 1 >= cur.s.len) vs[x][h] &= 0xffffu;
+                        }
                     }
                 }
-                uint32_t pb[NT][2];
+                uint32_t pb[NT][2][2];
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    float x[4];
+                    float y[2][4], most = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = fmaf(s[j][e], sc[j][e & 1], -m[j][e & 1]);
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            y[x][e] = fmaf(s[j][x][e], sc[j][e & 1], -m[j][e & 1]);
+                            most = fmaxf(most, y[x][e]);
+                        }
                     // the reference maximum moves when a score is more than 2^8 above it
-                    if (__any_sync(0xffffffffu, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) > 8.f)) {
+                    if (__any_sync(0xffffffffu, most > 8.f)) {
 #pragma unroll
                         for (int b = 0; b < 2; ++b) {
-                            float top = fmaxf(s[j][b], s[j][2 + b]) * sc[j][b];
+                            float top = fmaxf(fmaxf(s[j][0][b], s[j][0][2 + b]), fmaxf(s[j][1][b], s[j][1][2 + b])) * sc[j][b];
                             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
@@ -365,56 +460,67 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                                 o[j][c][b] *= alpha;
                                 o[j][c][2 + b] *= alpha;
                             }
-                            x[b] = fmaf(s[j][b], sc[j][b], -to);
-                            x[2 + b] = fmaf(s[j][2 + b], sc[j][b], -to);
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                y[x][b] = fmaf(s[j][x][b], sc[j][b], -to);
+                                y[x][2 + b] = fmaf(s[j][x][2 + b], sc[j][b], -to);
+                            }
                         }
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = fast_exp2(x[e]);
-                    l[j][0] += x[0] + x[2];
-                    l[j][1] += x[1] + x[3];
-                    pb[j][0] = transposed(pack_f16x2(x[0], x[1]));
-                    pb[j][1] = transposed(pack_f16x2(x[2], x[3]));
+                    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[x][e] = fast_exp2(y[x][e]);
+                        pb[j][x][0] = transposed(pack_f16x2(y[x][0], y[x][1]));
+                        pb[j][x][1] = transposed(pack_f16x2(y[x][2], y[x][3]));
+                    }
+                    l[j][0] += (y[0][0] + y[0][2]) + (y[1][0] + y[1][2]);
+                    l[j][1] += (y[0][1] + y[0][3]) + (y[1][1] + y[1][3]);
                 }
                 // O^T: elements 16 g + 2 i, + 1 (8 g at head_dim 64) of keys 2 t, 2 t + 1 and those 8 further on
-                uint32_t vw[2][2][kWords / 2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (D == 128) {
-                        const uint4 v = *reinterpret_cast<const uint4*>(tile + 8 * D + h * 512 + lane * 16);
-                        vw[h][0][0] = v.x; vw[h][0][kWords / 2 - 1] = v.y; vw[h][1][0] = v.z; vw[h][1][kWords / 2 - 1] = v.w;
-                    } else {
-                        const uint2 v = *reinterpret_cast<const uint2*>(tile + 8 * D + h * 256 + lane * 8);
-                        vw[h][0][0] = v.x; vw[h][1][0] = v.y;
-                    }
-                }
-#pragma unroll
-                for (int w = 0; w < kWords / 2; ++w) {
-                    uint32_t a[2][2][4];  // [keys][even, odd element]
+                for (int x = 0; x < 2; ++x) {
+                    const uint8_t* const tile = step + x * L::kTileBytes;
+                    uint32_t vw[2][2][kWords / 2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const uint32_t x = vw[h][0][w], y = vw[h][1][w];
-                        halves_of_word((x & 0x0f0f0f0fu) | (y << 4 & 0xf0f0f0f0u), a[h][0]);
-                        halves_of_word((x >> 4 & 0x0f0f0f0fu) | (y & 0xf0f0f0f0u), a[h][1]);
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) {
-                            a[h][0][b] = mul_f16x2(a[h][0][b], vs[h]);
-                            a[h][1][b] = mul_f16x2(a[h][1][b], vs[h]);
+                        if (D == 128) {
+                            const uint4 v = *reinterpret_cast<const uint4*>(tile + 8 * D + h * 512 + lane * 16);
+                            vw[h][0][0] = v.x; vw[h][0][kWords / 2 - 1] = v.y; vw[h][1][0] = v.z; vw[h][1][kWords / 2 - 1] = v.w;
+                        } else {
+                            const uint2 v = *reinterpret_cast<const uint2*>(tile + 8 * D + h * 256 + lane * 8);
+                            vw[h][0][0] = v.x; vw[h][1][0] = v.y;
                         }
                     }
 #pragma unroll
-                    for (int b = 0; b < 4; ++b)
+                    for (int w = 0; w < kWords / 2; ++w) {
+                        uint32_t a[2][2][4];  // [keys][even, odd element]
 #pragma unroll
-                        for (int j = 0; j < NT; ++j) mma16816_f16(o[j][4 * w + b], a[0][0][b], a[0][1][b], a[1][0][b], a[1][1][b], pb[j][0], pb[j][1]);
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t lo = vw[h][0][w], hi = vw[h][1][w];
+                            halves_of_word((lo & 0x0f0f0f0fu) | (hi << 4 & 0xf0f0f0f0u), a[h][0]);
+                            halves_of_word((lo >> 4 & 0x0f0f0f0fu) | (hi & 0xf0f0f0f0u), a[h][1]);
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) {
+                                a[h][0][b] = mul_f16x2(a[h][0][b], vs[x][h]);
+                                a[h][1][b] = mul_f16x2(a[h][1][b], vs[x][h]);
+                            }
+                        }
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+#pragma unroll
+                            for (int j = 0; j < NT; ++j) mma16816_f16(o[j][4 * w + b], a[0][0][b], a[0][1][b], a[1][0][b], a[1][1][b], pb[j][x][0], pb[j][x][1]);
+                    }
                 }
                 __syncwarp();  // every lane has read the place before it is filled again
             }
+            cur.t += tiles;
+            done_tiles += tiles;
 
             // ------------------------------------------------ its end
             const bool whole = first_tile == 0 && cur.t == cur.s.cnt;
-            const bool from_start = i == tiles;  // the part begins with it
-            const int slot = 2 * warp + (from_start ? 0 : 1);
-            float* const share = shares + slot * L::kShareFloats;
+            const int slot = 2 * warp + (done_tiles == tiles ? 0 : 1);  // the part begins with it, or ends with it
+            float* const share = share_at(slot);
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -445,10 +551,10 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                         }
                     }
                 }
-            if (!whole && lane == 0) s_share[slot] = {unit0, unit0 + cur.s.cnt, cur.r, cur.head, cur.chunk, cur.s.row0, cur.s.n, from_start};
+            if (!whole && lane == 0) s_share[slot] = {unit0, unit0 + cur.s.cnt, cur.r, cur.head, cur.chunk, cur.s.row0, cur.s.n};
             if (cur.t == cur.s.cnt) {
                 unit0 += cur.s.cnt;
-                if (i < mine) cur.next_unit(p, L::kRows);
+                if (done_tiles < mine) cur.next_unit(p, L::kRows);
             }
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -456,8 +562,10 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
     __syncthreads();
 
     // ---------------------------------------------------- shares of one unit stand one after another
-    const int64_t cta_lo = part_start(min(static_cast<int>(blockIdx.x) * W, n_workers), total, max(n_workers, 1));
-    const int64_t cta_hi = part_start(min(static_cast<int>(blockIdx.x + 1) * W, n_workers), total, max(n_workers, 1));
+    const int workers = max(part.n_workers, 1);
+    const int64_t cta_lo = part_start(min(static_cast<int>(blockIdx.x) * W, part.n_workers), part.total, workers);
+    const int64_t cta_hi = part_start(min(static_cast<int>(blockIdx.x + 1) * W, part.n_workers), part.total, workers);
+    PackedJoin join{0, 0, 0, 0, 0, 0};
     for (int a = 0; a < 2 * W; ++a) {
         if (s_share[a].u1 < 0) continue;
         const Share u = s_share[a];
@@ -466,17 +574,19 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
         const bool done = u.u0 >= cta_lo && u.u1 <= cta_hi;
         const int rows = min(u.n * p.G - u.chunk * L::kRows, L::kRows);
         // the place in the workspace: the first if this CTA's part begins with the unit
-        float* const part = p.part + (2 * static_cast<int64_t>(blockIdx.x) + (u.u0 <= cta_lo ? 0 : 1)) * L::kShareFloats;
+        const int second = u.u0 > cta_lo;
+        float* const left = p.part + (2 * static_cast<int64_t>(blockIdx.x) + second) * L::kShareFloats;
+        if (!done && u.u0 >= cta_lo) join = {worker_of(u.u1 - 1, part.total, workers) / W, second, u.row0, u.n, u.head, u.chunk};
         for (int x = threadIdx.x; x < rows * (D / 4); x += W * 32) {
             const int row = x / (D / 4), c = x % (D / 4);
             float top = kNoMax;
             for (int b = a; b < end; ++b)
-                if (s_share[b].u1 >= 0) top = fmaxf(top, shares[b * L::kShareFloats + L::kRows * D + row]);
+                if (s_share[b].u1 >= 0) top = fmaxf(top, share_at(b)[L::kRows * D + row]);
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
             float sum = 0.f;
             for (int b = a; b < end; ++b) {
                 if (s_share[b].u1 < 0) continue;
-                const float* const share = shares + b * L::kShareFloats;
+                const float* const share = share_at(b);
                 const float f = fast_exp2(share[L::kRows * D + row] - top);
                 const float4 v = reinterpret_cast<const float4*>(share + row * D)[c];
                 sum += f * share[L::kRows * (D + 1) + row];
@@ -488,15 +598,16 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                 reinterpret_cast<uint2*>(p.o + at.o)[c] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
                 if (c == 0 && p.lse) p.lse[at.lse] = sum > 0.f ? (top + log2f(sum)) * 0.693147180559945309f : -INFINITY;
             } else {
-                reinterpret_cast<float4*>(part + row * D)[c] = acc;
+                reinterpret_cast<float4*>(left + row * D)[c] = acc;
                 if (c == 0) {
-                    part[L::kRows * D + row] = top;
-                    part[L::kRows * (D + 1) + row] = sum;
+                    left[L::kRows * D + row] = top;
+                    left[L::kRows * (D + 1) + row] = sum;
                 }
             }
         }
         a = end - 1;
     }
+    if (threadIdx.x == 0) p.joins[blockIdx.x] = join;
 }
 
 // Units that cross from one CTA into the next: block (c, row) takes the one that CTA c - the first of it - ends with.  Lanes are
@@ -504,31 +615,17 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
 constexpr int kPackedMergeWarps = 8;
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kPackedMergeWarps * 32) packed_merge_kernel(const __grid_constant__ PackedAttnParams p, int ctas) {
+__global__ void __launch_bounds__(kPackedMergeWarps * 32) packed_merge_kernel(const __grid_constant__ PackedAttnParams p) {
     using L = PackedAttnLayout<D, NT>;
-    constexpr int W = L::kWarps;
     __shared__ float4 s_acc[kPackedMergeWarps][32];
     __shared__ float2 s_ml[kPackedMergeWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y, c0 = blockIdx.x;
     grid_wait();
     grid_launch_dependents();
-    int seq = 0;
-    int64_t before = 0;
-    const int64_t total = find_seq(p, L::kRows, -1, seq, before);
-    if (total == 0) return;
-    const int n_workers = workers_for(total, ctas * W);
-    const int c0 = blockIdx.x;
-    if ((c0 + 1) * W >= n_workers) return;  // nothing behind it
-    const int64_t lo = part_start(c0 * W, total, n_workers), hi = part_start((c0 + 1) * W, total, n_workers);
-    find_seq(p, L::kRows, hi - 1, seq, before);
-    PackedCursor cur;
-    cur.at(p, L::kRows, seq, hi - 1 - before);
-    const int64_t u0 = hi - 1 - cur.t, u1 = u0 + cur.s.cnt;
-    if (u1 <= hi || u0 < lo) return;  // ends here, or began before
-    const int rows = min(cur.s.n * p.G - cur.chunk * L::kRows, L::kRows);
-    if (row >= rows) return;
-    const int c1 = worker_of(u1 - 1, total, n_workers) / W;
-    auto share_of = [&](int c) { return p.part + (2 * static_cast<int64_t>(c) + (c == c0 && u0 > lo ? 1 : 0)) * L::kShareFloats; };
+    const PackedJoin join = p.joins[c0];
+    const int c1 = join.last;
+    if (c1 <= c0 || row >= min(join.n * p.G - join.chunk * L::kRows, L::kRows)) return;
+    auto share_of = [&](int c) { return p.part + (2 * static_cast<int64_t>(c) + (c == c0 ? join.second : 0)) * L::kShareFloats; };
     float top = kNoMax;
     for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(share_of(c) + L::kRows * D + row));
 #pragma unroll
@@ -554,7 +651,7 @@ __global__ void __launch_bounds__(kPackedMergeWarps * 32) packed_merge_kernel(co
         acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
         sum += s_ml[w].y;
     }
-    const PackedRow at = packed_row(p, cur.s.row0, cur.head, cur.chunk * L::kRows + row, D);
+    const PackedRow at = packed_row(p, join.row0, join.head, join.chunk * L::kRows + row, D);
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     if (lane < D / 4) reinterpret_cast<uint2*>(p.o + at.o)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     if (lane == 0 && p.lse) p.lse[at.lse] = sum > 0.f ? (top + log2f(sum)) * 0.693147180559945309f : -INFINITY;
@@ -565,10 +662,10 @@ static cudaError_t launch_rows(const PackedAttnParams& p, cudaStream_t stream) {
     using L = PackedAttnLayout<D, NT>;
     const cudaError_t e = launch_chained<packed_attn_kernel<D, NT>>(dim3(kNumSms), L::kWarps * 32, L::kTotal, stream, p);
     if (e != cudaSuccess) return e;
-    return launch_chained<packed_merge_kernel<D, NT>>(dim3(kNumSms - 1, L::kRows), kPackedMergeWarps * 32, 0, stream, p, kNumSms);
+    return launch_chained<packed_merge_kernel<D, NT>>(dim3(kNumSms - 1, L::kRows), kPackedMergeWarps * 32, 0, stream, p);
 }
 
-size_t packed_attn_workspace_bytes(int head_dim) { return 2 * static_cast<size_t>(kNumSms) * 16 * (head_dim + 2) * 4; }
+size_t packed_attn_workspace_bytes(int head_dim) { return sizeof(PackedJoin) * kNumSms + 2 * static_cast<size_t>(kNumSms) * 16 * (head_dim + 2) * 4; }
 
 cudaError_t launch_packed_attn(const PackedAttnParams& p, int head_dim, int max_rows, cudaStream_t stream) {
     const bool two = static_cast<int64_t>(max_rows) * p.G > 8;
