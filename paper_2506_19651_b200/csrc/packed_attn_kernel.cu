@@ -65,11 +65,28 @@ __device__ __forceinline__ PackedSeq packed_seq(const PackedAttnParams& p, int r
     return s;
 }
 
-// Where the part of warp w of the launch begins, of n_workers warps and all `total` tiles.
-__device__ __forceinline__ int64_t part_start(int64_t w, int64_t total, int n_workers) { return w * total / n_workers; }
-// The warp whose part a tile is in.
-__device__ __forceinline__ int worker_of(int64_t tile, int64_t total, int n_workers) { return static_cast<int>(((tile + 1) * n_workers - 1) / total); }
-__device__ __forceinline__ int workers_for(int64_t total, int most) { return static_cast<int>(min(static_cast<int64_t>(most), (total + 1) / 2)); }
+// a / b for a >= 0, b > 0: 32 bits wherever they do (a 64-bit division is a subroutine of a hundred instructions).
+__device__ __forceinline__ int64_t divided(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
+// How `total` tiles are dealt to n workers: the first `more` of them have each + 1 tiles, the others each.
+struct PackedDeal {
+    int64_t total, each;
+    int n, more;
+    __device__ __forceinline__ PackedDeal(int64_t tiles, int most) {
+        total = tiles;
+        n = static_cast<int>(min(static_cast<int64_t>(most), (tiles + 1) / 2));
+        each = n > 0 ? divided(tiles, n) : 0;
+        more = static_cast<int>(tiles - each * n);
+    }
+    __device__ __forceinline__ int64_t start(int w) const { return w < n ? w * each + min(w, more) : total; }
+    __device__ __forceinline__ int worker_of(int64_t tile) const {
+        const int64_t head = more * (each + 1);
+        return static_cast<int>(tile < head ? divided(tile, each + 1) : more + divided(tile - head, each));
+    }
+};
 
 __device__ __forceinline__ int64_t seq_tiles(const PackedAttnParams& p, int r, int rows_per_chunk) {
     if (r >= p.num_seqs) return 0;
@@ -86,32 +103,33 @@ __device__ __forceinline__ int64_t warp_inclusive(int64_t x) {
     return x;
 }
 
-// The calling warp's part of the list: tiles [lo, hi) of `total`, beginning `off` tiles into those of sequence seq.
+// The calling warp's part of the list begins `off` tiles into those of sequence seq.
 struct PackedPart {
-    int64_t total, lo, hi, off;
-    int seq, n_workers;
+    PackedDeal deal;
+    int64_t off;
+    int seq;
+    PackedSeq s;  // that sequence
 };
 
 template <int W>
 __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int rows_per_chunk) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, me = blockIdx.x * W + warp;
-    PackedPart part;
-    part.seq = 0;
-    part.off = 0;
-    auto bounds = [&](int64_t total) {
-        part.total = total;
-        part.n_workers = workers_for(total, gridDim.x * W);
-        part.lo = me < part.n_workers ? part_start(me, total, part.n_workers) : total;
-        part.hi = me < part.n_workers ? part_start(me + 1, total, part.n_workers) : total;
-    };
-    if (p.num_seqs <= 32) {  // each warp for itself
-        const int64_t mine = seq_tiles(p, lane, rows_per_chunk), to = warp_inclusive(mine);
-        bounds(__shfl_sync(0xffffffffu, to, 31));
-        const unsigned past = __ballot_sync(0xffffffffu, to > part.lo);
-        if (past) {
-            part.seq = __ffs(past) - 1;
-            part.off = part.lo - __shfl_sync(0xffffffffu, to - mine, part.seq);
-        }
+    if (p.num_seqs <= 32) {  // each warp for itself, a lane for every sequence
+        PackedSeq s{0, 0, 0, 0, 1, 0, 0};
+        if (lane < p.num_seqs) s = packed_seq(p, lane, rows_per_chunk);
+        const int64_t mine = static_cast<int64_t>(s.chunks) * s.cnt * p.Hkv, to = warp_inclusive(mine);
+        PackedPart part{PackedDeal(__shfl_sync(0xffffffffu, to, 31), gridDim.x * W), 0, 0, s};
+        const int64_t lo = part.deal.start(me);
+        const int seq = max(__ffs(__ballot_sync(0xffffffffu, to > lo)) - 1, 0);
+        part.seq = seq;
+        part.off = lo - __shfl_sync(0xffffffffu, to - mine, seq);
+        part.s.len = __shfl_sync(0xffffffffu, s.len, seq);
+        part.s.n = __shfl_sync(0xffffffffu, s.n, seq);
+        part.s.row0 = __shfl_sync(0xffffffffu, s.row0, seq);
+        part.s.chunks = __shfl_sync(0xffffffffu, s.chunks, seq);
+        part.s.cnt = __shfl_sync(0xffffffffu, s.cnt, seq);
+        part.s.ns = __shfl_sync(0xffffffffu, s.ns, seq);
+        part.s.skip = __shfl_sync(0xffffffffu, s.skip, seq);
         return part;
     }
     // a thread for every sequence, W * 32 at a time
@@ -125,7 +143,7 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
     int64_t total = 0;
 #pragma unroll
     for (int w = 0; w < W; ++w) total += s_sum[w];
-    bounds(total);
+    PackedPart part{PackedDeal(total, gridDim.x * W), 0, 0, {}};
     int64_t base = 0;
     for (int r0 = 0; r0 < p.num_seqs; r0 += W * 32) {
         const int r = r0 + threadIdx.x;
@@ -141,23 +159,23 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
             all += s_sum[w];
         }
         to += base;
-        if (mine > 0) {
+        const int64_t from = to - mine;
+        if (from < part.deal.start(blockIdx.x * W + W) && to > part.deal.start(blockIdx.x * W)) {
             for (int w = 0; w < W; ++w) {
-                const int worker = blockIdx.x * W + w;
-                if (worker >= part.n_workers) break;
-                const int64_t lo = part_start(worker, total, part.n_workers);
-                if (lo >= to - mine && lo < to) {
+                const int64_t lo = part.deal.start(blockIdx.x * W + w);
+                if (lo >= from && lo < to) {
                     s_seq[w] = r;
-                    s_off[w] = lo - (to - mine);
+                    s_off[w] = lo - from;
                 }
             }
         }
         base += all;
     }
     __syncthreads();
-    if (part.hi > part.lo) {
+    if (part.deal.start(me) < total) {
         part.seq = s_seq[warp];
         part.off = s_off[warp];
+        part.s = packed_seq(p, part.seq, rows_per_chunk);
     }
     return part;
 }
@@ -166,12 +184,10 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
 struct PackedCursor {
     PackedSeq s;
     int r, head, chunk, t;
-    __device__ __forceinline__ void at(const PackedAttnParams& p, int rows_per_chunk, int seq, int64_t off) {
-        r = seq;
-        s = packed_seq(p, r, rows_per_chunk);
-        const int64_t unit = off / s.cnt;
-        t = static_cast<int>(off - unit * s.cnt);
-        head = static_cast<int>(unit / s.chunks);
+    __device__ __forceinline__ explicit PackedCursor(const PackedPart& part) : s(part.s), r(part.seq) {
+        const int64_t unit = divided(part.off, s.cnt);
+        t = static_cast<int>(part.off - unit * s.cnt);
+        head = static_cast<int>(divided(unit, s.chunks));
         chunk = static_cast<int>(unit - static_cast<int64_t>(head) * s.chunks);
     }
     __device__ __forceinline__ void next_unit(const PackedAttnParams& p, int rows_per_chunk) {
@@ -186,6 +202,12 @@ struct PackedCursor {
         } while (s.chunks == 0);
     }
     __device__ __forceinline__ int key0(int x) const { return (x < s.ns ? x : x + s.skip) << 4; }
+    // Tiles [from, to) of the unit, of whose keys every row at positions pos_min .. pos_max sees all.
+    __device__ __forceinline__ void open_tiles(const PackedAttnParams& p, int pos_min, int pos_max, int& from, int& to) const {
+        from = 0;
+        to = max((pos_min + 1) >> 4, 0) - s.skip;
+        if (p.window > 0) from = max(((pos_max - p.window + 16) >> 4) - s.skip, s.ns);  // the sink's few are looked at one by one
+    }
     // Where tile x of the unit stands in the cache, in units of 128 bytes (which tile_units of them make); kNoTile where there is nothing to read.
     __device__ __forceinline__ uint32_t place(const PackedAttnParams& p, int x, int tile_units) const {
         const int tile = x < s.ns ? x : x + s.skip;
@@ -260,67 +282,23 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
     grid_wait();
 
     const PackedPart part = my_part<W>(p, L::kRows);
-    const int mine = static_cast<int>(part.hi - part.lo);
+    const PackedDeal& deal = part.deal;
+    const int64_t lo = deal.start(blockIdx.x * W + warp);
+    const int mine = static_cast<int>(deal.start(blockIdx.x * W + warp + 1) - lo);
     grid_launch_dependents();
     if (mine > 0) {
-        PackedCursor cur, ahead;
-        cur.at(p, L::kRows, part.seq, part.off);
-        ahead = cur;
+        PackedCursor cur(part), ahead(cur);
         // Fetching: steps of two tiles.  A lane holds the place of a tile, 32 tiles at a time and the 32 behind them, so that a page
         // is looked up long before it is needed.
         int to_fetch = mine, left = min(ahead.s.cnt - ahead.t, to_fetch);  // of the part, and of it in this unit
-        int block = ahead.t;
-        uint32_t places = ahead.place(p, block + lane, L::kTileBytes / 128), places_next = ahead.place(p, block + 32 + lane, L::kTileBytes / 128);
-        unsigned there = 0;  // two bits a place in the ring: the tiles exist
-        int stage_in = 0;
-        auto fetch = [&]() {
-            if (to_fetch > 0) {
-                if (ahead.t - block == 32) {
-                    block += 32;
-                    places = places_next;
-                    places_next = ahead.place(p, block + 32 + lane, L::kTileBytes / 128);
-                }
-                const uint32_t at0 = __shfl_sync(0xffffffffu, places, ahead.t - block), at1 = left > 1 ? __shfl_sync(0xffffffffu, places, ahead.t - block + 1) : kNoTile;
-                there = (there & ~(3u << (2 * stage_in))) | ((at0 != kNoTile ? 1u : 0u) | (at1 != kNoTile ? 2u : 0u)) << (2 * stage_in);
-                const uint8_t* const src0 = p.cache + static_cast<uint64_t>(at0) * 128 + lane * 16;
-                const uint8_t* const src1 = p.cache + static_cast<uint64_t>(at1) * 128 + lane * 16 - kChunks % 32 * 16;
-                const uint32_t dst = ring + stage_in * L::kStepBytes + lane * 16;
-                // the chunks of both tiles, 32 at a time: those in the middle are of one or the other (kChunks % 32 = 16 or 8)
-#pragma unroll
-                for (int c = 0; c < (2 * kChunks + 31) / 32; ++c) {
-                    const bool first = c * 32 + lane < kChunks;
-                    const uint8_t* const src = first ? src0 + c * 512 : src1 + (c - kChunks / 32) * 512;
-                    const bool some = (first ? at0 : at1) != kNoTile && ((c + 1) * 32 <= 2 * kChunks || c * 32 + lane < 2 * kChunks);
-                    if (some) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c * 512), "l"(src) : "memory");
-                }
-                stage_in = stage_in + 1 == L::kStages ? 0 : stage_in + 1;
-                const int step = min(left, 2);
-                to_fetch -= step;
-                left -= step;
-                ahead.t += step;
-                if (left == 0 && to_fetch > 0) {
-                    ahead.next_unit(p, L::kRows);
-                    left = min(ahead.s.cnt, to_fetch);
-                    block = 0;
-                    places = ahead.place(p, lane, L::kTileBytes / 128);
-                    places_next = ahead.place(p, 32 + lane, L::kTileBytes / 128);
-                }
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        for (int i = 0; i < L::kStages - 1; ++i) fetch();
-
-        int64_t unit0 = part.lo - cur.t;  // of this unit on the list
-        int stage = 0, done_tiles = 0;
-        while (done_tiles < mine) {
-            // ------------------------------------------------ a unit, or the share of it that is in this part
-            const int first_tile = cur.t, tiles = min(cur.s.cnt - cur.t, mine - done_tiles);
+        int in_block = 0;                                                  // of 32 places
+        uint32_t places = ahead.place(p, ahead.t + lane, L::kTileBytes / 128), places_next = ahead.place(p, ahead.t + 32 + lane, L::kTileBytes / 128);
+        // Rows of the unit: Q's fragments, the softmax scale in units of log2 and the positions of rows 2 t and 2 t + 1.
+        uint32_t q[NT][KS][2];
+        float sc[NT][2];
+        int pos[NT][2];
+        auto rows_of_unit = [&]() {
             const int rows = min(cur.s.n * p.G - cur.chunk * L::kRows, L::kRows);
-            uint32_t q[NT][KS][2];
-            float sc[NT][2];                // softmax scale, in units of log2, of rows 2 t and 2 t + 1
-            int pos[NT][2];
-            float m[NT][2], l[NT][2], o[NT][MT][4];
-            int pos_min = INT32_MAX, pos_max = -1;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 const int rr = cur.chunk * L::kRows + 8 * j + g;
@@ -350,23 +328,85 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                     sc[j][b] = __shfl_sync(0xffffffffu, up, 8 * t + 4 * b);
                     const int row = 8 * j + 2 * t + b;
                     pos[j][b] = row < rows ? cur.s.len - cur.s.n + quotient(cur.chunk * L::kRows + row, p.div_g) : -1;
+                }
+            }
+        };
+        rows_of_unit();  // the first ones while the first places are looked up
+        unsigned there = 0;  // two bits a step, the latest in the lowest: the tiles exist
+        const uint8_t* const cache = p.cache + lane * 16;
+        uint32_t into = 0;   // place in the ring
+        auto fetch = [&]() {
+            there <<= 2;
+            if (to_fetch > 0) {
+                const uint32_t at0 = __shfl_sync(0xffffffffu, places, in_block);
+                uint32_t at1 = __shfl_sync(0xffffffffu, places, in_block + 1);
+                if (left == 1) at1 = kNoTile;
+                there |= (at0 != kNoTile ? 1u : 0u) | (at1 != kNoTile ? 2u : 0u);
+                const uint8_t* const src0 = cache + static_cast<uint64_t>(at0) * 128;
+                const uint8_t* const src1 = cache + static_cast<uint64_t>(at1) * 128 - kChunks % 32 * 16;
+                const uint32_t dst = ring + lane * 16 + into;
+                // the chunks of both tiles, 32 at a time: those in the middle are of one or the other (kChunks % 32 = 16 or 8)
+#pragma unroll
+                for (int c = 0; c < (2 * kChunks + 31) / 32; ++c) {
+                    const bool first = c < kChunks / 32 || (c == kChunks / 32 && lane < kChunks % 32);
+                    const uint8_t* const src = first ? src0 + c * 512 : src1 + (c - kChunks / 32) * 512;
+                    const bool some = (first ? at0 : at1) != kNoTile && ((c + 1) * 32 <= 2 * kChunks || c * 32 + lane < 2 * kChunks);
+                    if (some) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c * 512), "l"(src) : "memory");
+                }
+                into = into + L::kStepBytes == L::kStages * L::kStepBytes ? 0 : into + L::kStepBytes;
+                in_block += 2;
+                left -= 2;
+                to_fetch -= 2;
+                if (left <= 0) {
+                    to_fetch -= left;  // a unit's last step may be one tile
+                    if (to_fetch > 0) {
+                        ahead.next_unit(p, L::kRows);
+                        left = min(ahead.s.cnt, to_fetch);
+                        in_block = 0;
+                        places = ahead.place(p, lane, L::kTileBytes / 128);
+                        places_next = ahead.place(p, 32 + lane, L::kTileBytes / 128);
+                    }
+                } else if (in_block == 32) {
+                    in_block = 0;
+                    ahead.t += 32;
+                    places = places_next;
+                    places_next = ahead.place(p, ahead.t + 32 + lane, L::kTileBytes / 128);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        for (int i = 0; i < L::kStages - 1; ++i) fetch();
+
+        int64_t unit0 = lo - cur.t;  // of this unit on the list
+        uint32_t from_place = 0;
+        int done_tiles = 0;
+        while (done_tiles < mine) {
+            // ------------------------------------------------ a unit, or the share of it that is in this part
+            const int first_tile = cur.t, tiles = min(cur.s.cnt - cur.t, mine - done_tiles);
+            const int rows = min(cur.s.n * p.G - cur.chunk * L::kRows, L::kRows);
+            float m[NT][2], l[NT][2], o[NT][MT][4];
+            if (done_tiles > 0) rows_of_unit();
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
                     m[j][b] = kNoMax;
                     l[j][b] = 0.f;
                 }
 #pragma unroll
                 for (int c = 0; c < MT; ++c) o[j][c][0] = o[j][c][1] = o[j][c][2] = o[j][c][3] = 0.f;
             }
-            pos_min = cur.s.len - cur.s.n + quotient(cur.chunk * L::kRows, p.div_g);
-            pos_max = cur.s.len - cur.s.n + quotient(cur.chunk * L::kRows + rows - 1, p.div_g);
-
-            for (int n = 0; n < tiles; n += 2) {
+            const int pos_min = cur.s.len - cur.s.n + quotient(cur.chunk * L::kRows, p.div_g);
+            const int pos_max = cur.s.len - cur.s.n + quotient(cur.chunk * L::kRows + rows - 1, p.div_g);
+            int open_from, open_to;
+            cur.open_tiles(p, pos_min, pos_max, open_from, open_to);
+            for (int n = first_tile; n < first_tile + tiles; n += 2) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
+                __syncwarp();  // this step is there for all lanes, and all have read the one before, whose place is filled again
+                const unsigned exist = there >> (2 * (L::kStages - 2)) & 3u;
                 fetch();
-                asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 1) : "memory");
-                __syncwarp();
-                const uint8_t* const step = my_ring + stage * L::kStepBytes;
-                const unsigned exist = there >> (2 * stage) & 3u;
-                stage = stage + 1 == L::kStages ? 0 : stage + 1;
-                const int key0[2] = {cur.key0(first_tile + n), cur.key0(first_tile + n + 1)};
+                const uint8_t* const step = my_ring + from_place;
+                from_place = from_place + L::kStepBytes == L::kStages * L::kStepBytes ? 0 : from_place + L::kStepBytes;
                 if (exist == 0) continue;
                 // S^T: keys g and g + 8 of either tile, rows 2 t and 2 t + 1
                 float s[NT][2][4];
@@ -414,8 +454,8 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                     vs[x][1] = scale_pair(vb >> 16);
                 }
                 // masks, and scales of 0 for what is behind the end or not there (its bytes may be anything)
-                const int last0 = max(key0[0], key0[1]);
-                if (exist != 3u || last0 + 15 > pos_min || (p.window > 0 && key0[0] <= pos_max - p.window && last0 + 15 >= p.sink)) {
+                if (exist != 3u || n < open_from || n + 1 >= open_to) {
+                    const int key0[2] = {cur.key0(n), cur.key0(n + 1)};
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         const bool is_there = exist >> x & 1;
@@ -512,8 +552,8 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                             for (int j = 0; j < NT; ++j) mma16816_f16(o[j][4 * w + b], a[0][0][b], a[0][1][b], a[1][0][b], a[1][1][b], pb[j][x][0], pb[j][x][1]);
                     }
                 }
-                __syncwarp();  // every lane has read the place before it is filled again
             }
+            __syncwarp();
             cur.t += tiles;
             done_tiles += tiles;
 
@@ -562,94 +602,123 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
     __syncthreads();
 
     // ---------------------------------------------------- shares of one unit stand one after another
-    const int workers = max(part.n_workers, 1);
-    const int64_t cta_lo = part_start(min(static_cast<int>(blockIdx.x) * W, part.n_workers), part.total, workers);
-    const int64_t cta_hi = part_start(min(static_cast<int>(blockIdx.x + 1) * W, part.n_workers), part.total, workers);
+    const int64_t cta_lo = deal.start(blockIdx.x * W), cta_hi = deal.start(blockIdx.x * W + W);
     PackedJoin join{0, 0, 0, 0, 0, 0};
-    for (int a = 0; a < 2 * W; ++a) {
-        if (s_share[a].u1 < 0) continue;
+    __shared__ float s_factor[2 * W][L::kRows];  // what each share of a row counts
+    __shared__ int s_list[2 * W];                // the shares of the unit
+    const int64_t u0_of = lane < 2 * W && s_share[lane].u1 >= 0 ? s_share[lane].u0 : -1;
+    unsigned left_over = __ballot_sync(0xffffffffu, u0_of >= 0);
+    while (left_over != 0) {
+        const int a = __ffs(left_over) - 1;
         const Share u = s_share[a];
-        int end = a + 1;
-        while (end < 2 * W && (s_share[end].u1 < 0 || s_share[end].u0 == u.u0)) ++end;
+        const unsigned group = __ballot_sync(0xffffffffu, u0_of == u.u0);
+        left_over &= ~group;
         const bool done = u.u0 >= cta_lo && u.u1 <= cta_hi;
-        const int rows = min(u.n * p.G - u.chunk * L::kRows, L::kRows);
+        const int rows = min(u.n * p.G - u.chunk * L::kRows, L::kRows), count = __popc(group);
         // the place in the workspace: the first if this CTA's part begins with the unit
         const int second = u.u0 > cta_lo;
         float* const left = p.part + (2 * static_cast<int64_t>(blockIdx.x) + second) * L::kShareFloats;
-        if (!done && u.u0 >= cta_lo) join = {worker_of(u.u1 - 1, part.total, workers) / W, second, u.row0, u.n, u.head, u.chunk};
-        for (int x = threadIdx.x; x < rows * (D / 4); x += W * 32) {
-            const int row = x / (D / 4), c = x % (D / 4);
-            float top = kNoMax;
-            for (int b = a; b < end; ++b)
-                if (s_share[b].u1 >= 0) top = fmaxf(top, share_at(b)[L::kRows * D + row]);
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            float sum = 0.f;
-            for (int b = a; b < end; ++b) {
-                if (s_share[b].u1 < 0) continue;
-                const float* const share = share_at(b);
-                const float f = fast_exp2(share[L::kRows * D + row] - top);
-                const float4 v = reinterpret_cast<const float4*>(share + row * D)[c];
-                sum += f * share[L::kRows * (D + 1) + row];
-                acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
-            }
-            if (done) {
-                const PackedRow at = packed_row(p, u.row0, u.head, u.chunk * L::kRows + row, D);
-                const float inv = sum > 0.f ? 1.f / sum : 0.f;
-                reinterpret_cast<uint2*>(p.o + at.o)[c] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-                if (c == 0 && p.lse) p.lse[at.lse] = sum > 0.f ? (top + log2f(sum)) * 0.693147180559945309f : -INFINITY;
-            } else {
-                reinterpret_cast<float4*>(left + row * D)[c] = acc;
-                if (c == 0) {
+        if (!done && u.u0 >= cta_lo) join = {deal.worker_of(u.u1 - 1) / W, second, u.row0, u.n, u.head, u.chunk};
+        // a warp for a row, a lane for a share
+        const bool in = group >> lane & 1;
+        const int at = __popc(group & ((1u << lane) - 1));
+        if (warp == 0 && in) s_list[at] = lane;
+        for (int row = warp; row < rows; row += W) {
+            const float m = in ? share_at(lane)[L::kRows * D + row] : kNoMax, l = in ? share_at(lane)[L::kRows * (D + 1) + row] : 0.f;
+            float top = m;
+#pragma unroll
+            for (int by = 16; by > 0; by /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, by));
+            const float f = fast_exp2(m - top);
+            float sum = f * l;
+#pragma unroll
+            for (int by = 16; by > 0; by /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, by);
+            if (in) s_factor[at][row] = done ? (sum > 0.f ? f / sum : 0.f) : f;
+            if (lane == 0) {
+                if (!done) {
                     left[L::kRows * D + row] = top;
                     left[L::kRows * (D + 1) + row] = sum;
+                } else if (p.lse) {
+                    p.lse[packed_row(p, u.row0, u.head, u.chunk * L::kRows + row, D).lse] = sum > 0.f ? (top + log2f(sum)) * 0.693147180559945309f : -INFINITY;
                 }
             }
         }
-        a = end - 1;
+        __syncthreads();
+        for (int x = threadIdx.x; x < rows * (D / 4); x += W * 32) {
+            const int row = x / (D / 4), c = x % (D / 4);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (int i = 0; i < count; ++i) {
+                const float f = s_factor[i][row];
+                const float4 v = reinterpret_cast<const float4*>(share_at(s_list[i]) + row * D)[c];
+                acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+            }
+            if (done)
+                reinterpret_cast<uint2*>(p.o + packed_row(p, u.row0, u.head, u.chunk * L::kRows + row, D).o)[c] = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+            else
+                reinterpret_cast<float4*>(left + row * D)[c] = acc;
+        }
+        __syncthreads();
     }
     if (threadIdx.x == 0) p.joins[blockIdx.x] = join;
 }
 
-// Units that cross from one CTA into the next: block (c, row) takes the one that CTA c - the first of it - ends with.  Lanes are
-// columns, the warps take the CTAs in turn and meet in shared memory.
-constexpr int kPackedMergeWarps = 8;
+// Units that cross from one CTA into the next: block c takes the one that CTA c - the first of it - ends with.  A warp for every row
+// and every fourth (second) of the CTAs, lanes are columns; the warps of a row meet in shared memory.
+constexpr int kPackedMergeWarps = 32;
 
 template <int D, int NT>
 __global__ void __launch_bounds__(kPackedMergeWarps * 32) packed_merge_kernel(const __grid_constant__ PackedAttnParams p) {
     using L = PackedAttnLayout<D, NT>;
-    __shared__ float4 s_acc[kPackedMergeWarps][32];
-    __shared__ float2 s_ml[kPackedMergeWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y, c0 = blockIdx.x;
+    constexpr int kTurns = kPackedMergeWarps / L::kRows;
+    __shared__ float4 s_acc[kTurns][L::kRows][32];
+    __shared__ float s_sum[kTurns][L::kRows];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = warp % L::kRows, turn = warp / L::kRows, c0 = blockIdx.x;
     grid_wait();
     grid_launch_dependents();
     const PackedJoin join = p.joins[c0];
     const int c1 = join.last;
-    if (c1 <= c0 || row >= min(join.n * p.G - join.chunk * L::kRows, L::kRows)) return;
+    if (c1 <= c0) return;
+    const bool some = row < min(join.n * p.G - join.chunk * L::kRows, L::kRows);
     auto share_of = [&](int c) { return p.part + (2 * static_cast<int64_t>(c) + (c == c0 ? join.second : 0)) * L::kShareFloats; };
-    float top = kNoMax;
-    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(share_of(c) + L::kRows * D + row));
-#pragma unroll
-    for (int by = 16; by > 0; by /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, by));
+    float top = kNoMax, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-#pragma unroll 4
-    for (int c = c0 + warp; c <= c1; c += kPackedMergeWarps) {
-        const float* const share = share_of(c);
-        const float f = fast_exp2(__ldcg(share + L::kRows * D + row) - top);
-        sum += f * __ldcg(share + L::kRows * (D + 1) + row);
-        if (lane < D / 4) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(share + row * D) + lane);
-            acc.x += f * v.x; acc.y += f * v.y; acc.z += f * v.z; acc.w += f * v.w;
+    if (some) {
+        constexpr int kAtOnce = 5;  // of a warp's shares, in flight together, with the first maxima
+        float4 v[kAtOnce];
+        float m[kAtOnce], l[kAtOnce];
+        auto load = [&](int first) {
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                const int c = min(first + i * kTurns, c1);
+                const float* const share = share_of(c);
+                m[i] = __ldcg(share + L::kRows * D + row);
+                l[i] = __ldcg(share + L::kRows * (D + 1) + row);
+                v[i] = __ldcg(reinterpret_cast<const float4*>(share + row * D) + lane % (D / 4));
+            }
+        };
+        load(c0 + turn);
+        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(share_of(c) + L::kRows * D + row));
+#pragma unroll
+        for (int by = 16; by > 0; by /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, by));
+        for (int c = c0 + turn; c <= c1; c += kAtOnce * kTurns) {
+            if (c > c0 + turn) load(c);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                const float f = c + i * kTurns <= c1 ? fast_exp2(m[i] - top) : 0.f;
+                sum += f * l[i];
+                acc.x += f * v[i].x; acc.y += f * v[i].y; acc.z += f * v[i].z; acc.w += f * v[i].w;
+            }
         }
     }
-    s_acc[warp][lane] = acc;
-    if (lane == 0) s_ml[warp] = make_float2(top, sum);
+    s_acc[turn][row][lane] = acc;
+    if (lane == 0) s_sum[turn][row] = sum;
     __syncthreads();
-    if (warp != 0) return;
-    for (int w = 1; w < kPackedMergeWarps; ++w) {
-        const float4 v = s_acc[w][lane];
+    if (turn != 0 || !some) return;
+#pragma unroll
+    for (int w = 1; w < kTurns; ++w) {
+        const float4 v = s_acc[w][row][lane];
         acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
-        sum += s_ml[w].y;
+        sum += s_sum[w][row];
     }
     const PackedRow at = packed_row(p, join.row0, join.head, join.chunk * L::kRows + row, D);
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
@@ -662,7 +731,7 @@ static cudaError_t launch_rows(const PackedAttnParams& p, cudaStream_t stream) {
     using L = PackedAttnLayout<D, NT>;
     const cudaError_t e = launch_chained<packed_attn_kernel<D, NT>>(dim3(kNumSms), L::kWarps * 32, L::kTotal, stream, p);
     if (e != cudaSuccess) return e;
-    return launch_chained<packed_merge_kernel<D, NT>>(dim3(kNumSms - 1, L::kRows), kPackedMergeWarps * 32, 0, stream, p);
+    return launch_chained<packed_merge_kernel<D, NT>>(dim3(kNumSms - 1), kPackedMergeWarps * 32, 0, stream, p);
 }
 
 size_t packed_attn_workspace_bytes(int head_dim) { return sizeof(PackedJoin) * kNumSms + 2 * static_cast<size_t>(kNumSms) * 16 * (head_dim + 2) * 4; }
