@@ -26,13 +26,17 @@
 
 namespace pevlm {
 
+// What a warp does at the start and the end of a unit takes it as long as so many tiles (measured: 1.9 us where a tile takes 0.7; 4.5 us
+// with 16 rows and heads of 64, a tile 0.46): they stand on the list in front of the unit's own, so that warps with several short units
+// have fewer tiles (64 sequences of 1 to 16K keys, one warp with five units: 64 us where the others took 55).
+constexpr int kUnitTiles = 4;
 constexpr uint32_t kNoTile = 0xffffffffu;
 constexpr float kNoMax = -3.0e38f;  // running maximum of a row that has seen no key: any score raises it
 
 template <int D, int NT>
 struct PackedAttnLayout {
-    static constexpr int kWarps = NT == 1 ? 12 : 8;
-    static constexpr int kStages = D == 128 ? 3 + (NT == 2) : 6;  // steps (two tiles) in a warp's ring
+    static constexpr int kWarps = D == 128 ? (NT == 1 ? 12 : 8) : (NT == 1 ? 16 : 12);  // as many as the registers allow, the same for each scheduler
+    static constexpr int kStages = D == 128 ? 3 + (NT == 2) : 5;  // steps (two tiles) in a warp's ring
     static constexpr int kTileBytes = 18 * D, kStepBytes = 2 * kTileBytes;
     static constexpr int kRows = 8 * NT;
     static constexpr int kShareFloats = kRows * (D + 2);          // O [rows][D], then m and l of each row
@@ -91,7 +95,7 @@ struct PackedDeal {
 __device__ __forceinline__ int64_t seq_tiles(const PackedAttnParams& p, int r, int rows_per_chunk) {
     if (r >= p.num_seqs) return 0;
     const PackedSeq s = packed_seq(p, r, rows_per_chunk);
-    return static_cast<int64_t>(s.chunks) * s.cnt * p.Hkv;
+    return static_cast<int64_t>(s.chunks) * (s.cnt + kUnitTiles) * p.Hkv;
 }
 
 __device__ __forceinline__ int64_t warp_inclusive(int64_t x) {
@@ -111,25 +115,47 @@ struct PackedPart {
     PackedSeq s;  // that sequence
 };
 
+constexpr int kSeqsPerLane = 4;  // up to 128 sequences are looked over by every warp for itself
+constexpr int kTableSeqs = 32 * kSeqsPerLane;
+
+// `table`: shared memory for the sequences' descriptions, where there are at most kTableSeqs (every warp writes the same).
 template <int W>
-__device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int rows_per_chunk) {
+__device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int rows_per_chunk, PackedSeq* table) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, me = blockIdx.x * W + warp;
-    if (p.num_seqs <= 32) {  // each warp for itself, a lane for every sequence
-        PackedSeq s{0, 0, 0, 0, 1, 0, 0};
-        if (lane < p.num_seqs) s = packed_seq(p, lane, rows_per_chunk);
-        const int64_t mine = static_cast<int64_t>(s.chunks) * s.cnt * p.Hkv, to = warp_inclusive(mine);
-        PackedPart part{PackedDeal(__shfl_sync(0xffffffffu, to, 31), gridDim.x * W), 0, 0, s};
+    if (p.num_seqs <= kTableSeqs) {  // each warp for itself, neighbouring sequences in a lane
+        const int each = (p.num_seqs + 31) / 32, r0 = lane * each;
+        PackedSeq s[kSeqsPerLane];
+        int64_t upto[kSeqsPerLane], mine = 0;
+#pragma unroll
+        for (int i = 0; i < kSeqsPerLane; ++i) {
+            s[i] = {0, 0, 0, 0, 1, 0, 0};
+            if (i < each && r0 + i < p.num_seqs) table[r0 + i] = s[i] = packed_seq(p, r0 + i, rows_per_chunk);
+            mine += static_cast<int64_t>(s[i].chunks) * (s[i].cnt + kUnitTiles) * p.Hkv;
+            upto[i] = mine;
+        }
+        const int64_t to = warp_inclusive(mine), from = to - mine;
+        PackedPart part{PackedDeal(__shfl_sync(0xffffffffu, to, 31), gridDim.x * W), 0, 0, s[0]};
         const int64_t lo = part.deal.start(me);
-        const int seq = max(__ffs(__ballot_sync(0xffffffffu, to > lo)) - 1, 0);
-        part.seq = seq;
-        part.off = lo - __shfl_sync(0xffffffffu, to - mine, seq);
-        part.s.len = __shfl_sync(0xffffffffu, s.len, seq);
-        part.s.n = __shfl_sync(0xffffffffu, s.n, seq);
-        part.s.row0 = __shfl_sync(0xffffffffu, s.row0, seq);
-        part.s.chunks = __shfl_sync(0xffffffffu, s.chunks, seq);
-        part.s.cnt = __shfl_sync(0xffffffffu, s.cnt, seq);
-        part.s.ns = __shfl_sync(0xffffffffu, s.ns, seq);
-        part.s.skip = __shfl_sync(0xffffffffu, s.skip, seq);
+        const int owner = max(__ffs(__ballot_sync(0xffffffffu, to > lo)) - 1, 0);
+        // in its owner's lane: which of its sequences
+        part.seq = r0;
+        part.off = lo - from;
+#pragma unroll
+        for (int i = 1; i < kSeqsPerLane; ++i)
+            if (lo - from >= upto[i - 1]) {
+                part.seq = r0 + i;
+                part.off = lo - from - upto[i - 1];
+                part.s = s[i];
+            }
+        part.seq = __shfl_sync(0xffffffffu, part.seq, owner);
+        part.off = __shfl_sync(0xffffffffu, part.off, owner);
+        part.s.len = __shfl_sync(0xffffffffu, part.s.len, owner);
+        part.s.n = __shfl_sync(0xffffffffu, part.s.n, owner);
+        part.s.row0 = __shfl_sync(0xffffffffu, part.s.row0, owner);
+        part.s.chunks = __shfl_sync(0xffffffffu, part.s.chunks, owner);
+        part.s.cnt = __shfl_sync(0xffffffffu, part.s.cnt, owner);
+        part.s.ns = __shfl_sync(0xffffffffu, part.s.ns, owner);
+        part.s.skip = __shfl_sync(0xffffffffu, part.s.skip, owner);
         return part;
     }
     // a thread for every sequence, W * 32 at a time
@@ -180,25 +206,26 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
     return part;
 }
 
-// A place on the list.
-struct PackedCursor {
+// A unit on the list.
+struct PackedUnit {
     PackedSeq s;
-    int r, head, chunk, t;
-    __device__ __forceinline__ explicit PackedCursor(const PackedPart& part) : s(part.s), r(part.seq) {
-        const int64_t unit = divided(part.off, s.cnt);
-        t = static_cast<int>(part.off - unit * s.cnt);
+    int r, head, chunk;
+    // The part's first one, and the part's first place in it.
+    __device__ __forceinline__ PackedUnit(const PackedPart& part, int& at) : s(part.s), r(part.seq) {
+        const int64_t unit = divided(part.off, s.cnt + kUnitTiles);
+        at = static_cast<int>(part.off - unit * (s.cnt + kUnitTiles));
         head = static_cast<int>(divided(unit, s.chunks));
         chunk = static_cast<int>(unit - static_cast<int64_t>(head) * s.chunks);
     }
-    __device__ __forceinline__ void next_unit(const PackedAttnParams& p, int rows_per_chunk) {
-        t = 0;
+    // The next one; past the last, r = num_seqs.
+    __device__ __forceinline__ void next(const PackedAttnParams& p, int rows_per_chunk, const PackedSeq* table) {
         if (++chunk < s.chunks) return;
         chunk = 0;
         if (++head < p.Hkv) return;
         head = 0;
         do {
             if (++r >= p.num_seqs) return;
-            s = packed_seq(p, r, rows_per_chunk);
+            s = p.num_seqs <= kTableSeqs ? table[r] : packed_seq(p, r, rows_per_chunk);
         } while (s.chunks == 0);
     }
     __device__ __forceinline__ int key0(int x) const { return (x < s.ns ? x : x + s.skip) << 4; }
@@ -208,11 +235,15 @@ struct PackedCursor {
         to = max((pos_min + 1) >> 4, 0) - s.skip;
         if (p.window > 0) from = max(((pos_max - p.window + 16) >> 4) - s.skip, s.ns);  // the sink's few are looked at one by one
     }
-    // Where tile x of the unit stands in the cache, in units of 128 bytes (which tile_units of them make); kNoTile where there is nothing to read.
-    __device__ __forceinline__ uint32_t place(const PackedAttnParams& p, int x, int tile_units) const {
+    // Page of tile x of the unit as the table has it (to be looked at only once it is needed: until then the load is in flight).
+    __device__ __forceinline__ int page(const PackedAttnParams& p, int x) const {
         const int tile = x < s.ns ? x : x + s.skip;
-        if (x >= s.cnt || tile << 4 >= s.len) return kNoTile;
-        const int page = __ldcg(p.page_table + static_cast<int64_t>(r) * p.max_pages + (tile >> (p.page_shift - 4)));
+        if (r >= p.num_seqs || x >= s.cnt || tile << 4 >= s.len) return -1;
+        return __ldcg(p.page_table + static_cast<int64_t>(r) * p.max_pages + (tile >> (p.page_shift - 4)));
+    }
+    // Where the tile stands in the cache, in units of 128 bytes (which tile_units of them make); kNoTile where there is nothing to read.
+    __device__ __forceinline__ uint32_t place(const PackedAttnParams& p, int x, int page, int tile_units) const {
+        const int tile = x < s.ns ? x : x + s.skip;
         if (page < 0 || page >= p.num_pages) return kNoTile;
         return static_cast<uint32_t>((((static_cast<int64_t>(page) * p.Hkv + head) << (p.page_shift - 4)) + (tile & ((1 << (p.page_shift - 4)) - 1))) * tile_units);
     }
@@ -281,18 +312,27 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
     __syncwarp();
     grid_wait();
 
-    const PackedPart part = my_part<W>(p, L::kRows);
+    __shared__ PackedSeq s_seqs[kTableSeqs];
+    const PackedPart part = my_part<W>(p, L::kRows, s_seqs);
     const PackedDeal& deal = part.deal;
-    const int64_t lo = deal.start(blockIdx.x * W + warp);
-    const int mine = static_cast<int>(deal.start(blockIdx.x * W + warp + 1) - lo);
+    const int64_t lo = deal.start(blockIdx.x * W + warp), hi = deal.start(blockIdx.x * W + warp + 1);
     grid_launch_dependents();
-    if (mine > 0) {
-        PackedCursor cur(part), ahead(cur);
-        // Fetching: steps of two tiles.  A lane holds the place of a tile, 32 tiles at a time and the 32 behind them, so that a page
-        // is looked up long before it is needed.
-        int to_fetch = mine, left = min(ahead.s.cnt - ahead.t, to_fetch);  // of the part, and of it in this unit
-        int in_block = 0;                                                  // of 32 places
-        uint32_t places = ahead.place(p, ahead.t + lane, L::kTileBytes / 128), places_next = ahead.place(p, ahead.t + 32 + lane, L::kTileBytes / 128);
+    if (lo < hi) {
+        // Fetching: steps of two tiles.  A lane holds the place of a tile, of 32 tiles, and the pages of the 32 behind them and of the
+        // first 32 of the next unit (`after`), so that a page is looked up long before it is needed.
+        int at;
+        PackedUnit cur(part, at), after(cur);
+        after.next(p, L::kRows, s_seqs);
+        constexpr int kUnits = L::kTileBytes / 128;
+        // Places [from, from + kUnitTiles) of the list belong to a unit, its tiles follow.  Those of it that are in the part:
+        int64_t unit0 = lo - at + kUnitTiles;  // of the unit's first tile
+        int first_tile = max(at - kUnitTiles, 0);
+        auto tiles_of = [&](const PackedUnit& u, int64_t tile0) { return static_cast<int>(max(min(hi - tile0, static_cast<int64_t>(u.s.cnt)), static_cast<int64_t>(0))); };
+        int64_t fetch0 = unit0;                          // the same of the unit that is fetched
+        int left = tiles_of(cur, fetch0) - first_tile;   // and its tiles that are yet to be
+        int in_block = 0, block = first_tile;            // of 32 places, and their first tile
+        PackedUnit ahead(cur);                           // the unit that is fetched
+        int page = ahead.page(p, block + lane), page_next = ahead.page(p, block + 32 + lane), page_after = after.page(p, lane);
         // Rows of the unit: Q's fragments, the softmax scale in units of log2 and the positions of rows 2 t and 2 t + 1.
         uint32_t q[NT][KS][2];
         float sc[NT][2];
@@ -308,7 +348,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                     const int tok = quotient(rr, p.div_g), h = cur.head * p.G + rr - tok * p.G;
                     const __nv_bfloat16* src = p.q + (cur.s.row0 + tok) * p.q_stride + h * D + t * (D / 4);
 #pragma unroll
-                    for (int c = 0; c < KS / 2; ++c) *reinterpret_cast<uint4*>(&x[4 * c]) = __ldcg(reinterpret_cast<const uint4*>(src) + c);
+                    for (int c = 0; c < KS / 2; ++c) *reinterpret_cast<uint4*>(&x[4 * c]) = reinterpret_cast<const uint4*>(src)[c];  // through L1: all warps of the SM read these rows
                 } else {
 #pragma unroll
                     for (int c = 0; c < KS * 2; ++c) x[c] = 0u;
@@ -331,13 +371,25 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                 }
             }
         };
+        // Q's rows of a unit that comes into L1, one line a lane
+        auto prefetch_rows = [&](const PackedUnit& u) {
+            constexpr int kLines = D / 64;
+            const int rows = min(u.s.n * p.G - u.chunk * L::kRows, L::kRows);
+#pragma unroll
+            for (int x = lane; x < L::kRows * kLines; x += 32) {
+                if (x / kLines >= rows) break;
+                const int rr = u.chunk * L::kRows + x / kLines, tok = quotient(rr, p.div_g), h = u.head * p.G + rr - tok * p.G;
+                asm volatile("prefetch.global.L1 [%0];" ::"l"(p.q + (u.s.row0 + tok) * p.q_stride + h * D + x % kLines * 64));
+            }
+        };
         rows_of_unit();  // the first ones while the first places are looked up
+        uint32_t places = ahead.place(p, block + lane, page, kUnits);
         unsigned there = 0;  // two bits a step, the latest in the lowest: the tiles exist
         const uint8_t* const cache = p.cache + lane * 16;
         uint32_t into = 0;   // place in the ring
         auto fetch = [&]() {
             there <<= 2;
-            if (to_fetch > 0) {
+            if (left > 0) {
                 const uint32_t at0 = __shfl_sync(0xffffffffu, places, in_block);
                 uint32_t at1 = __shfl_sync(0xffffffffu, places, in_block + 1);
                 if (left == 1) at1 = kNoTile;
@@ -356,36 +408,37 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                 into = into + L::kStepBytes == L::kStages * L::kStepBytes ? 0 : into + L::kStepBytes;
                 in_block += 2;
                 left -= 2;
-                to_fetch -= 2;
                 if (left <= 0) {
-                    to_fetch -= left;  // a unit's last step may be one tile
-                    if (to_fetch > 0) {
-                        ahead.next_unit(p, L::kRows);
-                        left = min(ahead.s.cnt, to_fetch);
-                        in_block = 0;
-                        places = ahead.place(p, lane, L::kTileBytes / 128);
-                        places_next = ahead.place(p, 32 + lane, L::kTileBytes / 128);
+                    fetch0 += ahead.s.cnt + kUnitTiles;
+                    if (fetch0 < hi) {
+                        ahead = after;
+                        left = tiles_of(ahead, fetch0);
+                        in_block = block = 0;
+                        places = ahead.place(p, lane, page_after, kUnits);
+                        page_next = ahead.page(p, 32 + lane);
+                        after.next(p, L::kRows, s_seqs);
+                        page_after = after.page(p, lane);
+                        prefetch_rows(ahead);
                     }
                 } else if (in_block == 32) {
                     in_block = 0;
-                    ahead.t += 32;
-                    places = places_next;
-                    places_next = ahead.place(p, ahead.t + 32 + lane, L::kTileBytes / 128);
+                    block += 32;
+                    places = ahead.place(p, block + lane, page_next, kUnits);
+                    page_next = ahead.page(p, block + 32 + lane);
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         for (int i = 0; i < L::kStages - 1; ++i) fetch();
 
-        int64_t unit0 = lo - cur.t;  // of this unit on the list
         uint32_t from_place = 0;
-        int done_tiles = 0;
-        while (done_tiles < mine) {
+        bool first_unit = true;
+        while (unit0 < hi) {
             // ------------------------------------------------ a unit, or the share of it that is in this part
-            const int first_tile = cur.t, tiles = min(cur.s.cnt - cur.t, mine - done_tiles);
+            const int tiles = tiles_of(cur, unit0) - first_tile;
             const int rows = min(cur.s.n * p.G - cur.chunk * L::kRows, L::kRows);
             float m[NT][2], l[NT][2], o[NT][MT][4];
-            if (done_tiles > 0) rows_of_unit();
+            if (!first_unit) rows_of_unit();
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
 #pragma unroll
@@ -554,12 +607,10 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                 }
             }
             __syncwarp();
-            cur.t += tiles;
-            done_tiles += tiles;
 
             // ------------------------------------------------ its end
-            const bool whole = first_tile == 0 && cur.t == cur.s.cnt;
-            const int slot = 2 * warp + (done_tiles == tiles ? 0 : 1);  // the part begins with it, or ends with it
+            const bool ends = first_tile + tiles == cur.s.cnt, whole = first_tile == 0 && ends;
+            const int slot = 2 * warp + (first_unit ? 0 : 1);  // the part begins with it, or ends with it
             float* const share = share_at(slot);
 #pragma unroll
             for (int j = 0; j < NT; ++j)
@@ -592,10 +643,10 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                     }
                 }
             if (!whole && lane == 0) s_share[slot] = {unit0, unit0 + cur.s.cnt, cur.r, cur.head, cur.chunk, cur.s.row0, cur.s.n};
-            if (cur.t == cur.s.cnt) {
-                unit0 += cur.s.cnt;
-                if (done_tiles < mine) cur.next_unit(p, L::kRows);
-            }
+            unit0 += cur.s.cnt + kUnitTiles;
+            first_unit = false;
+            first_tile = 0;
+            cur.next(p, L::kRows, s_seqs);
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
@@ -662,17 +713,18 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
     if (threadIdx.x == 0) p.joins[blockIdx.x] = join;
 }
 
-// Units that cross from one CTA into the next: block c takes the one that CTA c - the first of it - ends with.  A warp for every row
-// and every fourth (second) of the CTAs, lanes are columns; the warps of a row meet in shared memory.
-constexpr int kPackedMergeWarps = 32;
+// Units that cross from one CTA into the next: blocks (c, y) take the one that CTA c - the first of it - ends with, half of its rows each.  A warp
+// for every row and every fourth of the CTAs, lanes are columns; the warps of a row meet in shared memory.
+constexpr int kPackedMergeTurns = 4;
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kPackedMergeWarps * 32) packed_merge_kernel(const __grid_constant__ PackedAttnParams p) {
+__global__ void __launch_bounds__(4 * NT * kPackedMergeTurns * 32) packed_merge_kernel(const __grid_constant__ PackedAttnParams p) {
     using L = PackedAttnLayout<D, NT>;
-    constexpr int kTurns = kPackedMergeWarps / L::kRows;
-    __shared__ float4 s_acc[kTurns][L::kRows][32];
-    __shared__ float s_sum[kTurns][L::kRows];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = warp % L::kRows, turn = warp / L::kRows, c0 = blockIdx.x;
+    constexpr int kTurns = kPackedMergeTurns, kPackedMergeRows = 4 * NT;
+    __shared__ float4 s_acc[kTurns][kPackedMergeRows][32];
+    __shared__ float s_sum[kTurns][kPackedMergeRows];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, at_row = warp % kPackedMergeRows, turn = warp / kPackedMergeRows, c0 = blockIdx.x;
+    const int row = blockIdx.y * kPackedMergeRows + at_row;
     grid_wait();
     grid_launch_dependents();
     const PackedJoin join = p.joins[c0];
@@ -710,15 +762,15 @@ __global__ void __launch_bounds__(kPackedMergeWarps * 32) packed_merge_kernel(co
             }
         }
     }
-    s_acc[turn][row][lane] = acc;
-    if (lane == 0) s_sum[turn][row] = sum;
+    s_acc[turn][at_row][lane] = acc;
+    if (lane == 0) s_sum[turn][at_row] = sum;
     __syncthreads();
     if (turn != 0 || !some) return;
 #pragma unroll
     for (int w = 1; w < kTurns; ++w) {
-        const float4 v = s_acc[w][row][lane];
+        const float4 v = s_acc[w][at_row][lane];
         acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
-        sum += s_sum[w][row];
+        sum += s_sum[w][at_row];
     }
     const PackedRow at = packed_row(p, join.row0, join.head, join.chunk * L::kRows + row, D);
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
@@ -731,7 +783,7 @@ static cudaError_t launch_rows(const PackedAttnParams& p, cudaStream_t stream) {
     using L = PackedAttnLayout<D, NT>;
     const cudaError_t e = launch_chained<packed_attn_kernel<D, NT>>(dim3(kNumSms), L::kWarps * 32, L::kTotal, stream, p);
     if (e != cudaSuccess) return e;
-    return launch_chained<packed_merge_kernel<D, NT>>(dim3(kNumSms - 1), kPackedMergeWarps * 32, 0, stream, p);
+    return launch_chained<packed_merge_kernel<D, NT>>(dim3(kNumSms - 1, 2), 4 * NT * kPackedMergeTurns * 32, 0, stream, p);
 }
 
 size_t packed_attn_workspace_bytes(int head_dim) { return sizeof(PackedJoin) * kNumSms + 2 * static_cast<size_t>(kNumSms) * 16 * (head_dim + 2) * 4; }
