@@ -18,8 +18,8 @@ CSRC = os.path.join(_DIR, "csrc")
 LIB = os.path.join(_DIR, "libpevlm.so")
 CALL = os.path.join(_DIR, "_pevlm_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cu", "rope_kernel.cu", "assemble_kernel.cu", "attn_kernel.cu", "decode_kernel.cu", "merge_kernel.cu", "query_noalloc.cu", "selftest.cu",
-           "pages_kernel.cu", "packed_kernel.cu", "packed_attn_kernel.cu", "packed_api.cu"]
-HEADERS = ["internal.h", "ptx.cuh", "pycall.c", os.path.join("..", "..", "include", "pevlm.h")]
+           "pages_kernel.cu", "packed_kernel.cu", "packed_attn_kernel.cu", "packed_tile_kernel.cu", "packed_api.cu"]
+HEADERS = ["internal.h", "ptx.cuh", "packed_list.cuh", "pycall.c", os.path.join("..", "..", "include", "pevlm.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-cudart", "static"]
 

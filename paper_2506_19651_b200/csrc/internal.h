@@ -234,8 +234,8 @@ cudaError_t launch_packed_store(const PackedRows& p, int head_dim, cudaStream_t 
 cudaError_t launch_packed_load(const PackedRows& p, int head_dim, cudaStream_t stream);
 
 // Attention over the packed cache (packed_attn_kernel.cu).
-struct __align__(16) PackedJoin {  // what CTA c of the launch leaves unfinished and is the first of
-    int32_t last;      // last CTA with a share of it; nothing to join where that is not behind c
+struct __align__(16) PackedJoin {  // what worker c of the launch leaves unfinished and is the first of
+    int32_t last;      // last worker with a share of it; nothing to join where that is not behind c
     int32_t second;    // c's own share stands in its second place
     int32_t row0, n, head, chunk;
 };
@@ -245,8 +245,9 @@ struct PackedAttnParams {
     const int32_t *page_table, *lens, *row_start;
     __nv_bfloat16* o;        // [n_rows, Hq, d]
     float* lse;              // [Hq, n_rows] or NULL
-    PackedJoin* joins;       // one for each CTA
-    float* part;             // shares of units that cross from one CTA into the next, two places for each CTA
+    PackedJoin* joins;       // one for each worker (a CTA, or a pair)
+    float* part;             // shares of units that cross from one worker into the next, two places for each
+    WorkspaceHeader* hdr;
     int64_t q_stride;
     int32_t n_rows, num_seqs, num_pages, max_pages, page_shift;
     int32_t Hq, Hkv, G;
@@ -254,8 +255,11 @@ struct PackedAttnParams {
     Divisor div_g;
     float scale_log2;        // softmax scale * log2(e)
 };
-size_t packed_attn_workspace_bytes(int head_dim);
-cudaError_t launch_packed_attn(const PackedAttnParams& p, int head_dim, int max_rows, cudaStream_t stream);
+// `rows`: most rows of one sequence and kv head.  Up to kPackedFewRows of them go to packed_attn_kernel, more to packed_tile_kernel.
+constexpr int kPackedFewRows = 32;
+size_t packed_attn_workspace_bytes(int head_dim, int64_t rows);
+cudaError_t launch_packed_attn(const PackedAttnParams& p, int head_dim, int64_t rows, cudaStream_t stream);
+cudaError_t launch_packed_tile(const PackedAttnParams& p, int head_dim, cudaStream_t stream);  // without its merge
 
 cudaError_t launch_rope(const RopeParams& p, int head_dim, cudaStream_t stream);
 // tokens of a group of such a call, heads of V counted (not part of the ABI: the tests ask for it)

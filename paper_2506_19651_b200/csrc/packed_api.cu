@@ -128,7 +128,7 @@ static int check_rows(const pevlm_shape_t* s, int64_t n_rows, int64_t max_rows) 
 
 size_t pevlm_packed_workspace_bytes(const pevlm_shape_t* s, const pevlm_pages_t* g, int64_t n_rows, int64_t max_rows) {
     if (check_packed(s, g) != PEVLM_OK || check_rows(s, n_rows, max_rows) != PEVLM_OK) return 0;
-    return kStatusBytes + packed_attn_workspace_bytes(s->head_dim);
+    return kStatusBytes + packed_attn_workspace_bytes(s->head_dim, max_rows * (s->num_q_heads / s->num_kv_heads));
 }
 
 int pevlm_packed_attn(const pevlm_shape_t* s, const pevlm_pages_t* g, int32_t window, const void* q, int64_t q_stride, const void* cache,
@@ -157,6 +157,7 @@ int pevlm_packed_attn(const pevlm_shape_t* s, const pevlm_pages_t* g, int32_t wi
     p.page_table = page_table; p.lens = lens; p.row_start = row_start;
     p.o = static_cast<__nv_bfloat16*>(o);
     p.lse = lse;
+    p.hdr = static_cast<WorkspaceHeader*>(workspace);
     p.joins = reinterpret_cast<PackedJoin*>(static_cast<uint8_t*>(workspace) + kStatusBytes);
     p.part = reinterpret_cast<float*>(p.joins + kNumSms);
     p.q_stride = q_stride;
@@ -167,7 +168,7 @@ int pevlm_packed_attn(const pevlm_shape_t* s, const pevlm_pages_t* g, int32_t wi
     p.sink = s->sink_len;
     p.div_g = make_divisor(p.G);
     p.scale_log2 = resolve_scale(s) * 1.4426950408889634f;
-    const cudaError_t e = launch_packed_attn(p, s->head_dim, static_cast<int>(max_rows), static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_packed_attn(p, s->head_dim, max_rows * p.G, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? PEVLM_OK : cuda_fail(e, "packed attention launch");
 }
 

@@ -21,17 +21,9 @@
 // Rows of Q are scaled by a power of two to at most 2 in magnitude, so that any bf16 values fit fp16 (what is below 2^-24 of the
 // row's largest is lost, far below fp32's rounding of the sum); sums, maxima and outputs are fp32.  Probabilities are rounded to fp16
 // (2^-11 of each; 2^-24 of the row's largest where smaller).
-#include "internal.h"
-#include "ptx.cuh"
+#include "packed_list.cuh"
 
 namespace pevlm {
-
-// What a warp does at the start and the end of a unit takes it as long as so many tiles (measured: 1.9 us where a tile takes 0.7; 4.5 us
-// with 16 rows and heads of 64, a tile 0.46): they stand on the list in front of the unit's own, so that warps with several short units
-// have fewer tiles (64 sequences of 1 to 16K keys, one warp with five units: 64 us where the others took 55).
-constexpr int kUnitTiles = 4;
-constexpr uint32_t kNoTile = 0xffffffffu;
-constexpr float kNoMax = -3.0e38f;  // running maximum of a row that has seen no key: any score raises it
 
 template <int D, int NT>
 struct PackedAttnLayout {
@@ -43,76 +35,6 @@ struct PackedAttnLayout {
     static constexpr int kRing = kWarps * kStages * kStepBytes;
     static constexpr int kTotal = kRing + kWarps * kShareFloats * 4;
     static_assert(kShareFloats * 4 <= kStages * kStepBytes, "the second share of a warp is left in its ring");
-};
-
-// One sequence of the call as the tiles see it.
-struct PackedSeq {
-    int len, n, row0;      // keys, rows, first row
-    int chunks, cnt;       // units of a kv head, tiles of a unit
-    int ns, skip;          // tiles from ns on are skip tiles further on in the sequence (between sink and window nobody looks)
-};
-
-__device__ __forceinline__ PackedSeq packed_seq(const PackedAttnParams& p, int r, int rows_per_chunk) {
-    PackedSeq s;
-    s.len = min(max(p.lens[r], 0), p.max_pages << p.page_shift);
-    s.row0 = min(max(p.row_start[r], 0), p.n_rows);
-    s.n = max(min(p.row_start[r + 1], p.n_rows) - s.row0, 0);
-    s.chunks = (s.n * p.G + rows_per_chunk - 1) / rows_per_chunk;
-    s.ns = s.skip = 0;
-    const int tiles = (s.len + 15) >> 4;
-    if (p.window > 0) {
-        s.ns = (min(p.sink, s.len) + 15) >> 4;
-        const int lo = max(s.len - s.n - p.window + 1, 0) >> 4;  // tile of the first key that the first row's window shows
-        s.skip = min(max(lo - s.ns, 0), tiles - s.ns);
-    }
-    s.cnt = max(tiles - s.skip, 1);  // a sequence without keys has a tile that nothing is visible in
-    return s;
-}
-
-// a / b for a >= 0, b > 0: 32 bits wherever they do (a 64-bit division is a subroutine of a hundred instructions).
-__device__ __forceinline__ int64_t divided(int64_t a, int64_t b) {
-    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
-    return a / b;
-}
-
-// How `total` tiles are dealt to n workers: the first `more` of them have each + 1 tiles, the others each.
-struct PackedDeal {
-    int64_t total, each;
-    int n, more;
-    __device__ __forceinline__ PackedDeal(int64_t tiles, int most) {
-        total = tiles;
-        n = static_cast<int>(min(static_cast<int64_t>(most), (tiles + 1) / 2));
-        each = n > 0 ? divided(tiles, n) : 0;
-        more = static_cast<int>(tiles - each * n);
-    }
-    __device__ __forceinline__ int64_t start(int w) const { return w < n ? w * each + min(w, more) : total; }
-    __device__ __forceinline__ int worker_of(int64_t tile) const {
-        const int64_t head = more * (each + 1);
-        return static_cast<int>(tile < head ? divided(tile, each + 1) : more + divided(tile - head, each));
-    }
-};
-
-__device__ __forceinline__ int64_t seq_tiles(const PackedAttnParams& p, int r, int rows_per_chunk) {
-    if (r >= p.num_seqs) return 0;
-    const PackedSeq s = packed_seq(p, r, rows_per_chunk);
-    return static_cast<int64_t>(s.chunks) * (s.cnt + kUnitTiles) * p.Hkv;
-}
-
-__device__ __forceinline__ int64_t warp_inclusive(int64_t x) {
-#pragma unroll
-    for (int by = 1; by < 32; by *= 2) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, x, by);
-        if ((threadIdx.x & 31) >= static_cast<unsigned>(by)) x += y;
-    }
-    return x;
-}
-
-// The calling warp's part of the list begins `off` tiles into those of sequence seq.
-struct PackedPart {
-    PackedDeal deal;
-    int64_t off;
-    int seq;
-    PackedSeq s;  // that sequence
 };
 
 constexpr int kSeqsPerLane = 4;  // up to 128 sequences are looked over by every warp for itself
@@ -129,8 +51,8 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
 #pragma unroll
         for (int i = 0; i < kSeqsPerLane; ++i) {
             s[i] = {0, 0, 0, 0, 1, 0, 0};
-            if (i < each && r0 + i < p.num_seqs) table[r0 + i] = s[i] = packed_seq(p, r0 + i, rows_per_chunk);
-            mine += static_cast<int64_t>(s[i].chunks) * (s[i].cnt + kUnitTiles) * p.Hkv;
+            if (i < each && r0 + i < p.num_seqs) table[r0 + i] = s[i] = packed_seq<4>(p, r0 + i, rows_per_chunk);
+            mine += seq_tiles<4>(p, s[i]);
             upto[i] = mine;
         }
         const int64_t to = warp_inclusive(mine), from = to - mine;
@@ -162,7 +84,7 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
     __shared__ int64_t s_sum[W], s_off[W];
     __shared__ int s_seq[W];
     int64_t sum = 0;
-    for (int r = threadIdx.x; r < p.num_seqs; r += W * 32) sum += seq_tiles(p, r, rows_per_chunk);
+    for (int r = threadIdx.x; r < p.num_seqs; r += W * 32) sum += seq_tiles<4>(p, packed_seq<4>(p, r, rows_per_chunk));
     sum = warp_inclusive(sum);
     if (lane == 31) s_sum[warp] = sum;
     __syncthreads();
@@ -173,7 +95,7 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
     int64_t base = 0;
     for (int r0 = 0; r0 < p.num_seqs; r0 += W * 32) {
         const int r = r0 + threadIdx.x;
-        const int64_t mine = seq_tiles(p, r, rows_per_chunk);
+        const int64_t mine = r < p.num_seqs ? seq_tiles<4>(p, packed_seq<4>(p, r, rows_per_chunk)) : 0;
         int64_t to = warp_inclusive(mine);
         __syncthreads();
         if (lane == 31) s_sum[warp] = to;
@@ -201,53 +123,10 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
     if (part.deal.start(me) < total) {
         part.seq = s_seq[warp];
         part.off = s_off[warp];
-        part.s = packed_seq(p, part.seq, rows_per_chunk);
+        part.s = packed_seq<4>(p, part.seq, rows_per_chunk);
     }
     return part;
 }
-
-// A unit on the list.
-struct PackedUnit {
-    PackedSeq s;
-    int r, head, chunk;
-    // The part's first one, and the part's first place in it.
-    __device__ __forceinline__ PackedUnit(const PackedPart& part, int& at) : s(part.s), r(part.seq) {
-        const int64_t unit = divided(part.off, s.cnt + kUnitTiles);
-        at = static_cast<int>(part.off - unit * (s.cnt + kUnitTiles));
-        head = static_cast<int>(divided(unit, s.chunks));
-        chunk = static_cast<int>(unit - static_cast<int64_t>(head) * s.chunks);
-    }
-    // The next one; past the last, r = num_seqs.
-    __device__ __forceinline__ void next(const PackedAttnParams& p, int rows_per_chunk, const PackedSeq* table) {
-        if (++chunk < s.chunks) return;
-        chunk = 0;
-        if (++head < p.Hkv) return;
-        head = 0;
-        do {
-            if (++r >= p.num_seqs) return;
-            s = p.num_seqs <= kTableSeqs ? table[r] : packed_seq(p, r, rows_per_chunk);
-        } while (s.chunks == 0);
-    }
-    __device__ __forceinline__ int key0(int x) const { return (x < s.ns ? x : x + s.skip) << 4; }
-    // Tiles [from, to) of the unit, of whose keys every row at positions pos_min .. pos_max sees all.
-    __device__ __forceinline__ void open_tiles(const PackedAttnParams& p, int pos_min, int pos_max, int& from, int& to) const {
-        from = 0;
-        to = max((pos_min + 1) >> 4, 0) - s.skip;
-        if (p.window > 0) from = max(((pos_max - p.window + 16) >> 4) - s.skip, s.ns);  // the sink's few are looked at one by one
-    }
-    // Page of tile x of the unit as the table has it (to be looked at only once it is needed: until then the load is in flight).
-    __device__ __forceinline__ int page(const PackedAttnParams& p, int x) const {
-        const int tile = x < s.ns ? x : x + s.skip;
-        if (r >= p.num_seqs || x >= s.cnt || tile << 4 >= s.len) return -1;
-        return __ldcg(p.page_table + static_cast<int64_t>(r) * p.max_pages + (tile >> (p.page_shift - 4)));
-    }
-    // Where the tile stands in the cache, in units of 128 bytes (which tile_units of them make); kNoTile where there is nothing to read.
-    __device__ __forceinline__ uint32_t place(const PackedAttnParams& p, int x, int page, int tile_units) const {
-        const int tile = x < s.ns ? x : x + s.skip;
-        if (page < 0 || page >= p.num_pages) return kNoTile;
-        return static_cast<uint32_t>((((static_cast<int64_t>(page) * p.Hkv + head) << (p.page_shift - 4)) + (tile & ((1 << (p.page_shift - 4)) - 1))) * tile_units);
-    }
-};
 
 __device__ __forceinline__ void mma16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -259,38 +138,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t m) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(m));
     return r;
 }
-// The eight codes of a word as four pairs of fp16, byte by byte.
-__device__ __forceinline__ void halves_of_word(uint32_t w, uint32_t (&h)[4]) {
-    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-        "mov.b32 {a, b, c, d}, %4;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
-        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
-}
-__device__ __forceinline__ uint32_t scale_pair(uint32_t two_bytes) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(two_bytes)));
-    return r;
-}
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-// Where row rr (of a sequence and kv head: token rr / G, head rr % G of the group) of the result goes.
-struct PackedRow {
-    int64_t o, lse;
-};
-__device__ __forceinline__ PackedRow packed_row(const PackedAttnParams& p, int row0, int head, int rr, int d) {
-    const int tok = quotient(rr, p.div_g), h = head * p.G + rr - tok * p.G;
-    return {(static_cast<int64_t>(row0 + tok) * p.Hq + h) * d, static_cast<int64_t>(h) * p.n_rows + row0 + tok};
-}
-
 template <int D, int NT>
 __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packed_attn_kernel(const __grid_constant__ PackedAttnParams p) {
     using L = PackedAttnLayout<D, NT>;
@@ -313,6 +160,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
     grid_wait();
 
     __shared__ PackedSeq s_seqs[kTableSeqs];
+    const PackedSeq* const table = p.num_seqs <= kTableSeqs ? s_seqs : nullptr;
     const PackedPart part = my_part<W>(p, L::kRows, s_seqs);
     const PackedDeal& deal = part.deal;
     const int64_t lo = deal.start(blockIdx.x * W + warp), hi = deal.start(blockIdx.x * W + warp + 1);
@@ -321,18 +169,19 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
         // Fetching: steps of two tiles.  A lane holds the place of a tile, of 32 tiles, and the pages of the 32 behind them and of the
         // first 32 of the next unit (`after`), so that a page is looked up long before it is needed.
         int at;
-        PackedUnit cur(part, at), after(cur);
-        after.next(p, L::kRows, s_seqs);
-        constexpr int kUnits = L::kTileBytes / 128;
-        // Places [from, from + kUnitTiles) of the list belong to a unit, its tiles follow.  Those of it that are in the part:
-        int64_t unit0 = lo - at + kUnitTiles;  // of the unit's first tile
-        int first_tile = max(at - kUnitTiles, 0);
-        auto tiles_of = [&](const PackedUnit& u, int64_t tile0) { return static_cast<int>(max(min(hi - tile0, static_cast<int64_t>(u.s.cnt)), static_cast<int64_t>(0))); };
+        PackedUnit<4> cur(part, at), after(cur);
+        after.next(p, L::kRows, table);
+        // Places [from, from + kUnitTiles<4>) of the list belong to a unit, its tiles follow.  Those of it that are in the part:
+        int64_t unit0 = lo - at + kUnitTiles<4>;  // of the unit's first tile
+        int first_tile = max(at - kUnitTiles<4>, 0);
+        auto tiles_of = [&](const PackedUnit<4>& u, int64_t tile0) { return static_cast<int>(max(min(hi - tile0, static_cast<int64_t>(u.s.cnt)), static_cast<int64_t>(0))); };
         int64_t fetch0 = unit0;                          // the same of the unit that is fetched
         int left = tiles_of(cur, fetch0) - first_tile;   // and its tiles that are yet to be
         int in_block = 0, block = first_tile;            // of 32 places, and their first tile
-        PackedUnit ahead(cur);                           // the unit that is fetched
-        int page = ahead.page(p, block + lane), page_next = ahead.page(p, block + 32 + lane), page_after = after.page(p, lane);
+        PackedUnit<4> ahead(cur);                           // the unit that is fetched
+        auto page_of = [&](const PackedUnit<4>& u, int x) { return u.r < p.num_seqs && x < u.s.cnt ? packed_page(p, u.r, u.s.len, u.key0(x) >> 4) : -1; };
+        auto place_of = [&](const PackedUnit<4>& u, int x, int page) { return packed_place(p, page, u.head, u.key0(x) >> 4, L::kTileBytes / 128); };
+        int page = page_of(ahead, block + lane), page_next = page_of(ahead, block + 32 + lane), page_after = page_of(after, lane);
         // Rows of the unit: Q's fragments, the softmax scale in units of log2 and the positions of rows 2 t and 2 t + 1.
         uint32_t q[NT][KS][2];
         float sc[NT][2];
@@ -372,7 +221,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
             }
         };
         // Q's rows of a unit that comes into L1, one line a lane
-        auto prefetch_rows = [&](const PackedUnit& u) {
+        auto prefetch_rows = [&](const PackedUnit<4>& u) {
             constexpr int kLines = D / 64;
             const int rows = min(u.s.n * p.G - u.chunk * L::kRows, L::kRows);
 #pragma unroll
@@ -383,7 +232,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
             }
         };
         rows_of_unit();  // the first ones while the first places are looked up
-        uint32_t places = ahead.place(p, block + lane, page, kUnits);
+        uint32_t places = place_of(ahead, block + lane, page);
         unsigned there = 0;  // two bits a step, the latest in the lowest: the tiles exist
         const uint8_t* const cache = p.cache + lane * 16;
         uint32_t into = 0;   // place in the ring
@@ -409,22 +258,22 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                 in_block += 2;
                 left -= 2;
                 if (left <= 0) {
-                    fetch0 += ahead.s.cnt + kUnitTiles;
+                    fetch0 += ahead.s.cnt + kUnitTiles<4>;
                     if (fetch0 < hi) {
                         ahead = after;
                         left = tiles_of(ahead, fetch0);
                         in_block = block = 0;
-                        places = ahead.place(p, lane, page_after, kUnits);
-                        page_next = ahead.page(p, 32 + lane);
-                        after.next(p, L::kRows, s_seqs);
-                        page_after = after.page(p, lane);
+                        places = place_of(ahead, lane, page_after);
+                        page_next = page_of(ahead, 32 + lane);
+                        after.next(p, L::kRows, table);
+                        page_after = page_of(after, lane);
                         prefetch_rows(ahead);
                     }
                 } else if (in_block == 32) {
                     in_block = 0;
                     block += 32;
-                    places = ahead.place(p, block + lane, page_next, kUnits);
-                    page_next = ahead.page(p, block + 32 + lane);
+                    places = place_of(ahead, block + lane, page_next);
+                    page_next = page_of(ahead, block + 32 + lane);
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
@@ -643,10 +492,10 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                     }
                 }
             if (!whole && lane == 0) s_share[slot] = {unit0, unit0 + cur.s.cnt, cur.r, cur.head, cur.chunk, cur.s.row0, cur.s.n};
-            unit0 += cur.s.cnt + kUnitTiles;
+            unit0 += cur.s.cnt + kUnitTiles<4>;
             first_unit = false;
             first_tile = 0;
-            cur.next(p, L::kRows, s_seqs);
+            cur.next(p, L::kRows, table);
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
@@ -711,27 +560,26 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
         __syncthreads();
     }
     if (threadIdx.x == 0) p.joins[blockIdx.x] = join;
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.hdr->status = p.hdr->detail = 0;  // of a call before
 }
 
-// Units that cross from one CTA into the next: blocks (c, y) take the one that CTA c - the first of it - ends with, half of its rows each.  A warp
-// for every row and every fourth of the CTAs, lanes are columns; the warps of a row meet in shared memory.
-constexpr int kPackedMergeTurns = 4;
-
-template <int D, int NT>
-__global__ void __launch_bounds__(4 * NT * kPackedMergeTurns * 32) packed_merge_kernel(const __grid_constant__ PackedAttnParams p) {
-    using L = PackedAttnLayout<D, NT>;
-    constexpr int kTurns = kPackedMergeTurns, kPackedMergeRows = 4 * NT;
-    __shared__ float4 s_acc[kTurns][kPackedMergeRows][32];
-    __shared__ float s_sum[kTurns][kPackedMergeRows];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, at_row = warp % kPackedMergeRows, turn = warp / kPackedMergeRows, c0 = blockIdx.x;
-    const int row = blockIdx.y * kPackedMergeRows + at_row;
+// Units that cross from one worker (a CTA of packed_attn_kernel, a pair of packed_tile_kernel) into the next: blocks (c, y) take the one
+// that worker c - the first of it - ends with, RPB of its rows each.  A warp for every row and every TURNS-th of the workers, lanes are
+// columns; the warps of a row meet in shared memory.
+template <int D, int ROWS, int RPB, int TURNS>
+__global__ void __launch_bounds__(RPB * TURNS * 32) packed_merge_kernel(const __grid_constant__ PackedAttnParams p) {
+    constexpr int kTurns = TURNS, kShareFloats = ROWS * (D + 2);
+    __shared__ float4 s_acc[kTurns][RPB][32];
+    __shared__ float s_sum[kTurns][RPB];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, at_row = warp % RPB, turn = warp / RPB, c0 = blockIdx.x;
+    const int row = blockIdx.y * RPB + at_row;
     grid_wait();
     grid_launch_dependents();
     const PackedJoin join = p.joins[c0];
     const int c1 = join.last;
     if (c1 <= c0) return;
-    const bool some = row < min(join.n * p.G - join.chunk * L::kRows, L::kRows);
-    auto share_of = [&](int c) { return p.part + (2 * static_cast<int64_t>(c) + (c == c0 ? join.second : 0)) * L::kShareFloats; };
+    const bool some = row < min(join.n * p.G - join.chunk * ROWS, ROWS);
+    auto share_of = [&](int c) { return p.part + (2 * static_cast<int64_t>(c) + (c == c0 ? join.second : 0)) * kShareFloats; };
     float top = kNoMax, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (some) {
@@ -743,13 +591,13 @@ __global__ void __launch_bounds__(4 * NT * kPackedMergeTurns * 32) packed_merge_
             for (int i = 0; i < kAtOnce; ++i) {
                 const int c = min(first + i * kTurns, c1);
                 const float* const share = share_of(c);
-                m[i] = __ldcg(share + L::kRows * D + row);
-                l[i] = __ldcg(share + L::kRows * (D + 1) + row);
+                m[i] = __ldcg(share + ROWS * D + row);
+                l[i] = __ldcg(share + ROWS * (D + 1) + row);
                 v[i] = __ldcg(reinterpret_cast<const float4*>(share + row * D) + lane % (D / 4));
             }
         };
         load(c0 + turn);
-        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(share_of(c) + L::kRows * D + row));
+        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(share_of(c) + ROWS * D + row));
 #pragma unroll
         for (int by = 16; by > 0; by /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, by));
         for (int c = c0 + turn; c <= c1; c += kAtOnce * kTurns) {
@@ -772,7 +620,7 @@ __global__ void __launch_bounds__(4 * NT * kPackedMergeTurns * 32) packed_merge_
         acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
         sum += s_sum[w][at_row];
     }
-    const PackedRow at = packed_row(p, join.row0, join.head, join.chunk * L::kRows + row, D);
+    const PackedRow at = packed_row(p, join.row0, join.head, join.chunk * ROWS + row, D);
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     if (lane < D / 4) reinterpret_cast<uint2*>(p.o + at.o)[lane] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     if (lane == 0 && p.lse) p.lse[at.lse] = sum > 0.f ? (top + log2f(sum)) * 0.693147180559945309f : -INFINITY;
@@ -783,15 +631,27 @@ static cudaError_t launch_rows(const PackedAttnParams& p, cudaStream_t stream) {
     using L = PackedAttnLayout<D, NT>;
     const cudaError_t e = launch_chained<packed_attn_kernel<D, NT>>(dim3(kNumSms), L::kWarps * 32, L::kTotal, stream, p);
     if (e != cudaSuccess) return e;
-    return launch_chained<packed_merge_kernel<D, NT>>(dim3(kNumSms - 1, 2), 4 * NT * kPackedMergeTurns * 32, 0, stream, p);
+    return launch_chained<packed_merge_kernel<D, 8 * NT, 4 * NT, 4>>(dim3(kNumSms - 1, 2), 16 * NT * 32, 0, stream, p);
 }
 
-size_t packed_attn_workspace_bytes(int head_dim) { return sizeof(PackedJoin) * kNumSms + 2 * static_cast<size_t>(kNumSms) * 16 * (head_dim + 2) * 4; }
+template <int D>
+static cudaError_t launch_tiles(const PackedAttnParams& p, cudaStream_t stream) {
+    const cudaError_t e = launch_packed_tile(p, D, stream);
+    if (e != cudaSuccess) return e;
+    return launch_chained<packed_merge_kernel<D, 2 * kTile, 8, 1>>(dim3(kNumSms / 2 - 1, 2 * kTile / 8), 8 * 32, 0, stream, p);
+}
 
-cudaError_t launch_packed_attn(const PackedAttnParams& p, int head_dim, int max_rows, cudaStream_t stream) {
-    const bool two = static_cast<int64_t>(max_rows) * p.G > 8;
-    if (head_dim == 128) return two ? launch_rows<128, 2>(p, stream) : launch_rows<128, 1>(p, stream);
-    return two ? launch_rows<64, 2>(p, stream) : launch_rows<64, 1>(p, stream);
+static bool takes_tiles(int64_t rows) { return rows > kPackedFewRows; }
+
+size_t packed_attn_workspace_bytes(int head_dim, int64_t rows) {
+    const int unit = takes_tiles(rows) ? kTile : 16;  // rows for each CTA
+    return sizeof(PackedJoin) * kNumSms + 2 * static_cast<size_t>(kNumSms) * unit * (head_dim + 2) * sizeof(float);
+}
+
+cudaError_t launch_packed_attn(const PackedAttnParams& p, int head_dim, int64_t rows, cudaStream_t stream) {
+    if (takes_tiles(rows)) return head_dim == 128 ? launch_tiles<128>(p, stream) : launch_tiles<64>(p, stream);
+    if (head_dim == 128) return rows > 8 ? launch_rows<128, 2>(p, stream) : launch_rows<128, 1>(p, stream);
+    return rows > 8 ? launch_rows<64, 2>(p, stream) : launch_rows<64, 1>(p, stream);
 }
 
 }  // namespace pevlm

@@ -91,7 +91,7 @@ class Case:
         ws.fill_(0xFF)
         pb.pevlm_packed_attn(self.shape, self.pages, self.window, self.q, self.cache, self.table, self.d_lens, self.start, self.n_rows, most,
                              o, lse, ws, self.stride)
-        torch.cuda.synchronize()
+        assert pb.pevlm_read_status(ws) == (0, 0)
         guard.check()
         return o, lse
 
@@ -162,6 +162,19 @@ CASES = {
     "large keys": dict(lens=[400], rows=[2], Hq=7, Hkv=1, d=128, P=16, k_scale=8.0),
     "small queries": dict(lens=[400], rows=[2], Hq=7, Hkv=1, d=128, P=16, q_scale=2.0 ** -100, k_scale=30.0),
     "large queries": dict(lens=[100], rows=[2], Hq=7, Hkv=1, d=64, P=16, q_scale=2.0 ** 40, scale=2.0 ** -43),
+    "40 rows": dict(lens=[129], rows=[40], Hq=2, Hkv=2, d=128, P=16),
+    "question, heads of 64": dict(lens=[1000, 127, 128, 129], rows=[50, 127, 128, 40], Hq=8, Hkv=2, d=64, P=16),
+    "question of a long cache": dict(lens=[9000], rows=[64], Hq=28, Hkv=4, d=128, P=64),
+    "questions of 300 and 1": dict(lens=[2500, 700, 1, 0, 300], rows=[300, 1, 1, 2, 300], Hq=7, Hkv=1, d=128, P=32),
+    "more question than cache": dict(lens=[100, 0, 30], rows=[400, 70, 50], Hq=4, Hkv=2, d=64, P=16),
+    "chunk of a prefill under a window": dict(lens=[3000, 900], rows=[700, 900], Hq=4, Hkv=1, d=128, P=64, window=150, sink=70),
+    "window, heads of 64, sink of two tiles": dict(lens=[1500], rows=[333], Hq=6, Hkv=2, d=64, P=32, window=260, sink=200),
+    "short window": dict(lens=[700], rows=[200], Hq=2, Hkv=1, d=64, P=16, window=3, sink=1),
+    "question, pages that are not there": dict(lens=[1100, 300], rows=[64, 40], Hq=4, Hkv=2, d=128, P=16, holes=[(0, 0), (0, 7), (0, 20), (0, 21), (0, 68), (1, 18)]),
+    "whole tiles that are not there": dict(lens=[900], rows=[90], Hq=4, Hkv=2, d=64, P=128, holes=[(0, 0), (0, 3), (0, 7)]),
+    "many questions": dict(lens=[(i * 53) % 400 for i in range(150)], rows=[(i * 7) % 60 for i in range(150)], Hq=4, Hkv=2, d=64, P=16),
+    "question, large keys": dict(lens=[600], rows=[64], Hq=7, Hkv=1, d=128, P=16, k_scale=8.0),
+    "question, small and strided queries": dict(lens=[500], rows=[64], Hq=4, Hkv=1, d=64, P=16, q_scale=2.0 ** -90, k_scale=20.0, stride=4 * 64 + 128, extra_rows=3),
     "scale": dict(lens=[100], rows=[1], Hq=4, Hkv=2, d=64, P=16, scale=0.5),
 }
 
@@ -172,24 +185,27 @@ def test_against_the_definition(name):
     c.check(*c.run())
 
 
-@pytest.mark.parametrize("name", ["drafted tokens", "a question", "page ends", "as many rows as keys"])
+@pytest.mark.parametrize("name", ["drafted tokens", "a question", "page ends", "as many rows as keys", "page ends, heads of 64", "no key among others", "window",
+                                  "pages that are not there", "many without rows", "sink longer than the sequence"])
 def test_any_row_hint_gives_a_right_result(name):
     """max_rows chooses the kernel; the row counts on the device are what is computed."""
     c = Case(**CASES[name], seed=3)
-    for most in (1, c.n_rows):
+    for most in (1, min(c.n_rows, 2), c.n_rows):
         c.check(*c.run(max_rows=most))
 
 
-def test_same_bits_twice_and_on_a_replayed_graph():
+@pytest.mark.parametrize("rows", [[1, 2, 1], [64, 3, 200]])
+def test_same_bits_twice_and_on_a_replayed_graph(rows):
     import torch
-    c = Case([3000, 17, 900], [1, 2, 1], 28, 4, 128, 64, seed=9)
+    c = Case([3000, 17, 900], rows, 28, 4, 128, 64, seed=9)
+    most = max(rows)
     o, lse = c.run()
     o2, lse2 = c.run()
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
     pb = c.pb
-    ws = torch.empty(pb.pevlm_packed_workspace_bytes(c.shape, c.pages, c.n_rows, 2), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(pb.pevlm_packed_workspace_bytes(c.shape, c.pages, c.n_rows, most), dtype=torch.uint8, device="cuda")
     o3, lse3 = torch.zeros_like(o), torch.zeros_like(lse)
-    call = lambda: pb.pevlm_packed_attn(c.shape, c.pages, 0, c.q, c.cache, c.table, c.d_lens, c.start, c.n_rows, 2, o3, lse3, ws)
+    call = lambda: pb.pevlm_packed_attn(c.shape, c.pages, 0, c.q, c.cache, c.table, c.d_lens, c.start, c.n_rows, most, o3, lse3, ws)
     side, graphs = torch.cuda.Stream(), []
     torch.cuda.synchronize()
     for _ in range(2):  # two graphs that share the workspace, replayed in turn
