@@ -80,6 +80,27 @@ __device__ __forceinline__ void mbar_wait_cluster(uint32_t bar, uint32_t parity,
     }
 }
 
+template <typename T>
+__device__ __forceinline__ T ld_shared(uint32_t addr) {
+    T x;
+    if constexpr (sizeof(T) == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(addr) : "memory");
+    else if constexpr (sizeof(T) == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(addr) : "memory");
+    else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
+    return x;
+}
+__device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
+    uint32_t x;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
+    return x;
+}
+// The eight codes of a word times a scale (twice in a word), as eight fp16 in shared memory.
+__device__ __forceinline__ void st_shared_values(uint32_t addr, uint32_t codes, uint32_t scale2) {
+    uint32_t x[4];
+    halves_of_word(codes, x);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(mul_f16x2(x[0], scale2)), "r"(mul_f16x2(x[1], scale2)), "r"(mul_f16x2(x[2], scale2)),
+                 "r"(mul_f16x2(x[3], scale2)) : "memory");
+}
+
 __device__ __forceinline__ int same_in_warp(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 // Between the two softmax warps of a scheduler, see attn_kernel.cu; no limit: both go through the same tiles whatever happens.
 __device__ __forceinline__ void turn_wait(int what, int wg, int quarter) { asm volatile("bar.sync %0, 64;" ::"r"(what + wg * 4 + quarter) : "memory"); }
@@ -439,96 +460,94 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive_release_cluster(q_bar);
+            // ---- the tiles.  A tile's codes are in registers before the tile before it is handed on, so that neither the fetch nor
+            // shared memory's latency stand between two tiles, and its place in the ring of packed tiles is free as soon as they are.
+            uint4 kc[2];            // K: codes of keys g and g + 8 of this warp's 16 (heads of 64: two words of each are used)
+            uint32_t ks = 0;        // and their scales
+            uint2 vc[2][2];         // V: codes of keys k8 and k8 + 8 of two parts of 16 keys
+            uint32_t vs[2][2];      // and their scale
+            unsigned there = 0;
+            auto load = [&](uint32_t u) {
+                const uint32_t place = u % kRawRing;
+                wait(bars.raw_full[place], (u / kRawRing) & 1, kTwRaw);
+                there = s_raw_there[place];
+                const uint32_t raw = smem_base + L::kRaw + place * L::kRawBytes;
+                const uint32_t sub = raw + (4 * rank + fw) * L::kSubBytes;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (D == 128) kc[h] = ld_shared<uint4>(sub + h * 512 + lane * 16);
+                    else *reinterpret_cast<uint2*>(&kc[h]) = ld_shared<uint2>(sub + h * 256 + lane * 8);
+                }
+                ks = D == 128 ? ld_shared<uint32_t>(sub + 16 * D + lane * 4) : ld_shared<uint32_t>(sub + 16 * D + (lane >> 1) * 4) >> (lane & 1) * 16;
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t v = raw + (2 * fw + s2) * L::kSubBytes;
+                        if (D == 128) vc[s2][h] = ld_shared<uint2>(v + 8 * D + ((h * 8 + eighth) * 8 + k8) * 8);
+                        else vc[s2][h].x = ld_shared<uint32_t>(v + 8 * D + ((h * 8 + eighth) * 8 + k8) * 4);
+                        vs[s2][h] = ld_shared_u8(v + 17 * D + (D == 128 ? eighth : eighth >> 1) * 16 + (k8 >> 1) * 4 + h * 2 + (k8 & 1));
+                    }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars.raw_free[place]));
+            };
+            // where this thread's chunks of 16 bytes go: eight lanes that store together hit all banks (of K's words the upper quarters of the head
+            // take theirs in another order)
+            const bool upper = D == 128 && c4 >= 2;
+            const uint32_t k_to = smem_base + L::kK + (upper ? L::kKPanelBytes : 0) + (fw * 16 + g) * 128;
+            const uint32_t k_chunk = D == 128 ? (4 * (c4 & 1)) ^ (upper ? 2 : 0) ^ g : (2 * c4) ^ g;
+            const uint32_t v_to = smem_base + L::kV + (fw * 32 + k8) * (D == 128 ? 128 : 64);
+            const uint32_t v_chunk = D == 128 ? (2 * e4) ^ k8 : e4 ^ (k8 >> 1);
+            load(t);
 #pragma unroll 1
             for (int j = 0; j < it.nt; ++j, ++t) {
-                const uint32_t slot = t % kFeedRing, place = t % kRawRing;
-                const uint8_t* const raw = smem + L::kRaw + place * L::kRawBytes;
-                wait(bars.raw_full[place], (t / kRawRing) & 1, kTwRaw);
-                const unsigned there = s_raw_there[place];
+                const uint32_t slot = t % kFeedRing;
+                if (t >= kFeedRing) {
+                    wait_s_full(t - kFeedRing, kTwKFree);
+                    wait_pv_done(t - kFeedRing, kTwVFree);
+                }
                 // ---- K: 16 keys a warp, those of this CTA
-                if (t >= kFeedRing) wait_s_full(t - kFeedRing, kTwKFree);
-                {
-                    const uint8_t* const sub = raw + (4 * rank + fw) * L::kSubBytes;
-                    uint8_t* const to = smem + L::kK + slot * L::kKBytes + (fw * 16 + g) * 128;
-                    if (D == 128) {
-                        const uint32_t sb = *reinterpret_cast<const uint32_t*>(sub + 16 * D + lane * 4);
+                const uint32_t k_at = k_to + slot * L::kKBytes;
+                if (D == 128) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint4 codes = *reinterpret_cast<const uint4*>(sub + h * 512 + lane * 16);
-                            const uint32_t two = scale_pair(sb >> (16 * h)), sc[2] = {__byte_perm(two, 0, 0x1010), __byte_perm(two, 0, 0x3232)};
-                            // eight lanes that store together take different chunks: the upper quarters their words in another order
-                            const bool upper = c4 >> 1;
-                            const uint32_t w[4] = {upper ? codes.z : codes.x, upper ? codes.w : codes.y, upper ? codes.x : codes.z, upper ? codes.y : codes.w};
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t two = scale_pair(ks >> (16 * h)), s0 = __byte_perm(two, 0, upper ? 0x3232 : 0x1010), s1 = __byte_perm(two, 0, upper ? 0x1010 : 0x3232);
+                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 0) << 4), upper ? kc[h].z : kc[h].x, s0);
+                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 1) << 4), upper ? kc[h].w : kc[h].y, s0);
+                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 2) << 4), upper ? kc[h].x : kc[h].z, s1);
+                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 3) << 4), upper ? kc[h].y : kc[h].w, s1);
+                    }
+                } else {
+                    const uint32_t two = scale_pair(ks);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                uint32_t x[4];
-                                halves_of_word(w[i], x);
-                                const uint32_t s = upper == static_cast<bool>(i >> 1) ? sc[0] : sc[1];
-                                const int chunk = 4 * (c4 & 1) + (i ^ (upper ? 2 : 0));
-                                *reinterpret_cast<uint4*>(to + (c4 >> 1) * L::kKPanelBytes + h * 8 * 128 + ((chunk ^ g) << 4)) =
-                                    make_uint4(mul_f16x2(x[0], s), mul_f16x2(x[1], s), mul_f16x2(x[2], s), mul_f16x2(x[3], s));
-                            }
-                        }
-                    } else {
-                        const uint32_t two = scale_pair(*reinterpret_cast<const uint16_t*>(sub + 16 * D + lane * 2));
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint2 codes = *reinterpret_cast<const uint2*>(sub + h * 256 + lane * 8);
-                            const uint32_t s = __byte_perm(two, 0, h ? 0x3232 : 0x1010), w[2] = {codes.x, codes.y};
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                uint32_t x[4];
-                                halves_of_word(w[i], x);
-                                *reinterpret_cast<uint4*>(to + h * 8 * 128 + (((2 * c4 + i) ^ g) << 4)) =
-                                    make_uint4(mul_f16x2(x[0], s), mul_f16x2(x[1], s), mul_f16x2(x[2], s), mul_f16x2(x[3], s));
-                            }
-                        }
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t s0 = __byte_perm(two, 0, h ? 0x3232 : 0x1010);
+                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 0) << 4), kc[h].x, s0);
+                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 1) << 4), kc[h].y, s0);
                     }
                 }
+                // ---- V: 32 keys a warp, this CTA's columns; zeros for keys behind the end or not there, whose bytes may be anything
+                const int key0 = ((it.t0 + j < it.ns) ? it.t0 + j : it.t0 + j + it.skip) << 7;
+                const uint32_t v_at = v_to + slot * L::kVBytes;
+                const bool clean = key0 + kTile <= it.len && there == 0xffu;
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t s = scale_pair(vs[s2][h] | vs[s2][h] << 8);
+                        if (!clean && (key0 + (2 * fw + s2) * 16 + h * 8 + k8 >= it.len || !(there >> (2 * fw + s2) & 1))) s = 0u;
+                        const uint32_t at = v_at + (s2 * 16 + h * 8) * (D == 128 ? 128 : 64);
+                        st_shared_values(at + (v_chunk << 4), vc[s2][h].x, s);
+                        if (D == 128) st_shared_values(at + ((v_chunk ^ 1) << 4), vc[s2][h].y, s);
+                    }
                 if (warp == 8 && lane == 0) s_there[t % kFedRing] = there;
+                if (j + 1 < it.nt) load(t + 1);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(smem_u32(&bars.fed[t % kFedRing]));
                     mbar_arrive_release_cluster(map_to_cta(smem_u32(&bars.k_full[slot]), 0));
-                }
-                // ---- V: 32 keys a warp, this CTA's columns; zeros for keys behind the end or not there, whose bytes may be anything
-                if (t >= kFeedRing) wait_pv_done(t - kFeedRing, kTwVFree);
-                const int key0 = ((it.t0 + j < it.ns) ? it.t0 + j : it.t0 + j + it.skip) << 7;
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) {
-                    const int part16 = 2 * fw + s2;
-                    const uint8_t* const sub = raw + part16 * L::kSubBytes;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int key = part16 * 16 + h * 8 + k8;
-                        const uint32_t b = sub[17 * D + (D == 128 ? eighth : eighth >> 1) * 16 + (k8 >> 1) * 4 + h * 2 + (k8 & 1)];
-                        uint32_t s = scale_pair(b | b << 8);
-                        if (key0 + key >= it.len || !(there >> part16 & 1)) s = 0u;
-                        uint8_t* const to = smem + L::kV + slot * L::kVBytes + key * (D == 128 ? 128 : 64);
-                        if (D == 128) {
-                            const uint2 codes = *reinterpret_cast<const uint2*>(sub + 8 * D + ((h * 8 + eighth) * 8 + k8) * 8);
-                            const uint32_t w[2] = {codes.x, codes.y};
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                uint32_t x[4];
-                                halves_of_word(w[i], x);
-                                *reinterpret_cast<uint4*>(to + (((2 * e4 + i) ^ k8) << 4)) =
-                                    make_uint4(mul_f16x2(x[0], s), mul_f16x2(x[1], s), mul_f16x2(x[2], s), mul_f16x2(x[3], s));
-                            }
-                        } else {
-                            uint32_t x[4];
-                            halves_of_word(*reinterpret_cast<const uint32_t*>(sub + 8 * D + ((h * 8 + eighth) * 8 + k8) * 4), x);
-                            *reinterpret_cast<uint4*>(to + ((e4 ^ (k8 >> 1)) << 4)) =
-                                make_uint4(mul_f16x2(x[0], s), mul_f16x2(x[1], s), mul_f16x2(x[2], s), mul_f16x2(x[3], s));
-                        }
-                    }
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
                     mbar_arrive_release_cluster(map_to_cta(smem_u32(&bars.v_full[slot]), 0));
-                    mbar_arrive(smem_u32(&bars.raw_free[place]));
                 }
                 // the item before is written out once this one's first tiles are on their way (no later: their PV needs the accumulator)
                 if (done.k >= 0 && j == min(1, it.nt - 1)) {
