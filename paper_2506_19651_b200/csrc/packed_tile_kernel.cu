@@ -5,7 +5,7 @@
 //   warps 0-3, 4-7  softmax, one thread per row
 //   warps 8-11  feeder: turns the CTA's half of every K tile (64 keys) and V tile (D/2 columns) from e2m1 codes and e4m3 scales into fp16 in
 //               the swizzled layout the MMAs read, brings Q's rows into it, and between two items writes out the finished one
-//   warps 12, 14 (first CTA of the pair) issue the MMAs, warp 13 fetches the packed tiles (cp.async.bulk, 16 tokens of a page each),
+//   warps 12, 14 (first CTA of the pair) issue the MMAs, warp 12 of the second hands its feeder's work over; warp 13 fetches the packed tiles (cp.async.bulk, 16 tokens of a page each),
 //   warp 15     makes the work items
 // Everything is fp16 instead of bf16: the cache's values are exact in it and two instructions a pair make them (a conversion and the product
 // with the scale; bf16 would take five); rows of Q are scaled by a power of two (see packed_attn_kernel.cu), whose inverse goes into the row's softmax
@@ -140,7 +140,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
     struct Bars {
         uint64_t item_full[kTileItems], item_free[kTileItems];  // both: each CTA has its own
         uint64_t raw_full[kRawRing], raw_free[kRawRing];        // both
-        uint64_t q_full, k_full[kFeedRing], v_full[kFeedRing];  // first: both CTAs have written theirs
+        uint64_t q_full, kv_full[kFeedRing];                    // both: the CTA's feeder has written; first: and the other's (see the hand-over)
         uint64_t q_free;                                        // both
         uint64_t fed[kFedRing];                                 // both: the tile's mask (and its item's scales) are there
         uint64_t s_full[kFeedRing], pv_done[kFeedRing];         // both: QK(t), PV(t) are complete
@@ -170,15 +170,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
         s_published = 0;
         for (int i = 0; i < kTileItems; ++i) {
             mbar_init(smem_u32(&bars.item_full[i]), 1);
-            mbar_init(smem_u32(&bars.item_free[i]), 1 + 8 + 4 + (rank == 0 ? 2 : 0));
+            mbar_init(smem_u32(&bars.item_free[i]), 1 + 8 + 4 + (rank == 0 ? 2 : 1));
         }
         for (int i = 0; i < kRawRing; ++i) {
             mbar_init(smem_u32(&bars.raw_full[i]), 1);
             mbar_init(smem_u32(&bars.raw_free[i]), 4);
         }
         for (int i = 0; i < kFeedRing; ++i) {
-            mbar_init(smem_u32(&bars.k_full[i]), 8);
-            mbar_init(smem_u32(&bars.v_full[i]), 8);
+            mbar_init(smem_u32(&bars.kv_full[i]), rank == 0 ? 4 + 1 : 4);
             mbar_init(smem_u32(&bars.s_full[i]), 1);
             mbar_init(smem_u32(&bars.pv_done[i]), 1);
         }
@@ -188,7 +187,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
         }
         for (int i = 0; i < kFedRing; ++i) mbar_init(smem_u32(&bars.fed[i]), 4);
         for (int i = 0; i < kTileSums; ++i) mbar_init(smem_u32(&bars.sums_full[i]), 8);
-        mbar_init(smem_u32(&bars.q_full), 8);
+        mbar_init(smem_u32(&bars.q_full), rank == 0 ? 4 + 1 : 4);
         mbar_init(smem_u32(&bars.q_free), 1);
         mbar_init(smem_u32(&bars.o_free), 8);
         fence_mbar_init();
@@ -323,7 +322,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
 #pragma unroll 1
                 for (int j = 0; j < nt; ++j, ++t) {
                     const uint32_t slot = t % kFeedRing;
-                    mbar_wait_cluster(smem_u32(&bars.k_full[slot]), (t / kFeedRing) & 1, wait_state, kTwK);
+                    mbar_wait_cluster(smem_u32(&bars.kv_full[slot]), (t / kFeedRing) & 1, wait_state, kTwK);
                     if (t >= 2) wait(bars.s_read[t & 1], ((t >> 1) - 1) & 1, kTwSRead);
                     tc_fence_after_sync();
                     mma_ss_batch<D / 16>(tmem_base + (t & 1) * kTile, q_lo, desc_lo(smem_base + L::kK + slot * L::kKBytes, 16),
@@ -331,6 +330,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                     mma_commit_pair(smem_u32(&bars.s_full[slot]));
                 }
                 mma_commit_pair(smem_u32(&bars.q_free));
+            }
+        } else if (warp == 12) {
+            // ------------------------------------------------------------- hand-over: tells the first CTA what the second's feeder has written
+            // (An arrival that releases this CTA's writes to the other one takes 650 cycles of the warp that makes it; two of them a tile in
+            // the feeder were half of its time.)
+            const uint32_t q_bar = map_to_cta(smem_u32(&bars.q_full), 0);
+            uint32_t t = 0;
+#pragma unroll 1
+            for (int k = 0; same_in_warp(item_ready(k)); ++k) {
+                const int nt = same_in_warp(s_items[k % kTileItems].nt);
+                __syncwarp();
+                if (lane == 0) item_release(k);
+                wait(bars.q_full, k & 1, kTwQ);
+                __syncwarp();
+                if (lane == 0) mbar_arrive_release_cluster(q_bar);
+#pragma unroll 1
+                for (int j = 0; j < nt; ++j, ++t) {
+                    wait(bars.kv_full[t % kFeedRing], (t / kFeedRing) & 1, kTwK);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_release_cluster(map_to_cta(smem_u32(&bars.kv_full[t % kFeedRing]), 0));
+                }
             }
         } else if (rank == 0 && warp == 14) {
             // ------------------------------------------------------------- O += P V of the pair
@@ -348,7 +368,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                     const uint32_t slot = t % kFeedRing;
                     const uint32_t v_lo = desc_lo(smem_base + L::kV + slot * L::kVBytes, 0);
                     const uint32_t a_tmem = tmem_base + kTileTmemP + (t & 1) * (kTile / 2);
-                    mbar_wait_cluster(smem_u32(&bars.v_full[slot]), (t / kFeedRing) & 1, wait_state, kTwV);
+                    mbar_wait_cluster(smem_u32(&bars.kv_full[slot]), (t / kFeedRing) & 1, wait_state, kTwV);
                     wait(bars.p_full[t & 1], (t >> 1) & 1, kTwP);
                     tc_fence_after_sync();
 #pragma unroll 1
@@ -365,7 +385,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
         const int eighth = 4 * static_cast<int>(rank) + e4;
         const int row = tid & 127;
         const uint32_t tO = tmem_base + kTileTmemO + (static_cast<uint32_t>(fw * 32) << 16);
-        const uint32_t q_bar = map_to_cta(smem_u32(&bars.q_full), 0), o_free_bar = map_to_cta(smem_u32(&bars.o_free), 0);
+        const uint32_t o_free_bar = map_to_cta(smem_u32(&bars.o_free), 0);
         uint32_t t = 0;
         struct Finished {
             int row0, n, head, chunk, whole, second, k;
@@ -459,7 +479,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive_release_cluster(q_bar);
+            if (lane == 0) mbar_arrive(smem_u32(&bars.q_full));
             // ---- the tiles.  A tile's codes are in registers before the tile before it is handed on, so that neither the fetch nor
             // shared memory's latency stand between two tiles, and its place in the ring of packed tiles is free as soon as they are.
             uint4 kc[2];            // K: codes of keys g and g + 8 of this warp's 16 (heads of 64: two words of each are used)
@@ -546,8 +566,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(smem_u32(&bars.fed[t % kFedRing]));
-                    mbar_arrive_release_cluster(map_to_cta(smem_u32(&bars.k_full[slot]), 0));
-                    mbar_arrive_release_cluster(map_to_cta(smem_u32(&bars.v_full[slot]), 0));
+                    mbar_arrive(smem_u32(&bars.kv_full[slot]));
                 }
                 // the item before is written out once this one's first tiles are on their way (no later: their PV needs the accumulator)
                 if (done.k >= 0 && j == min(1, it.nt - 1)) {
