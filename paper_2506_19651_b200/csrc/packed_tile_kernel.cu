@@ -24,7 +24,8 @@ constexpr int kFeedRing = 4;     // K tiles and V tiles in fp16
 constexpr int kFedRing = 8;      // tiles whose masks are kept: the feeder may be four tiles ahead of a softmax warp that has yet to look
 constexpr int kRawRing = 3;      // packed tiles in flight
 constexpr int kTileItems = 4;    // work items in flight
-constexpr int kTileSums = 3;     // items whose row sums may be in flight between softmax and epilogue
+constexpr int kTileSums = 4;     // items whose row sums may be in flight between softmax and epilogue (a softmax warp that has no tile in an
+                                 // item leaves its sums at once: up to three items of one tile ahead of the one that is written out)
 constexpr int kTileTurn = 40;    // see kTurn in attn_kernel.cu
 constexpr float kTileRescaleLog2 = 8.0f;
 constexpr uint32_t kTileTmemP = 2 * kTile, kTileTmemO = 3 * kTile;
@@ -88,17 +89,12 @@ __device__ __forceinline__ T ld_shared(uint32_t addr) {
     else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
     return x;
 }
-__device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
-    uint32_t x;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
-    return x;
-}
 // The eight codes of a word times a scale (twice in a word), as eight fp16 in shared memory.
 __device__ __forceinline__ void st_shared_values(uint32_t addr, uint32_t codes, uint32_t scale2) {
     uint32_t x[4];
     halves_of_word(codes, x);
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(mul_f16x2(x[0], scale2)), "r"(mul_f16x2(x[1], scale2)), "r"(mul_f16x2(x[2], scale2)),
-                 "r"(mul_f16x2(x[3], scale2)) : "memory");
+                 "r"(mul_f16x2(x[3], scale2)));  // (ordered by the fence behind a tile's stores, and free to mix with one another's conversions)
 }
 
 __device__ __forceinline__ int same_in_warp(int x) { return __shfl_sync(0xffffffffu, x, 0); }
@@ -140,7 +136,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
     struct Bars {
         uint64_t item_full[kTileItems], item_free[kTileItems];  // both: each CTA has its own
         uint64_t raw_full[kRawRing], raw_free[kRawRing];        // both
-        uint64_t q_full, kv_full[kFeedRing];                    // both: the CTA's feeder has written; first: and the other's (see the hand-over)
+        uint64_t q_full, k_full[kFeedRing], v_full[kFeedRing];  // both: the CTA's feeder has written; first: and the other's (see the hand-over)
         uint64_t q_free;                                        // both
         uint64_t fed[kFedRing];                                 // both: the tile's mask (and its item's scales) are there
         uint64_t s_full[kFeedRing], pv_done[kFeedRing];         // both: QK(t), PV(t) are complete
@@ -170,14 +166,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
         s_published = 0;
         for (int i = 0; i < kTileItems; ++i) {
             mbar_init(smem_u32(&bars.item_full[i]), 1);
-            mbar_init(smem_u32(&bars.item_free[i]), 1 + 8 + 4 + (rank == 0 ? 2 : 1));
+            mbar_init(smem_u32(&bars.item_free[i]), 1 + 8 + 4 + 2);
         }
         for (int i = 0; i < kRawRing; ++i) {
             mbar_init(smem_u32(&bars.raw_full[i]), 1);
             mbar_init(smem_u32(&bars.raw_free[i]), 4);
         }
         for (int i = 0; i < kFeedRing; ++i) {
-            mbar_init(smem_u32(&bars.kv_full[i]), rank == 0 ? 4 + 1 : 4);
+            mbar_init(smem_u32(&bars.k_full[i]), rank == 0 ? 4 + 1 : 4);
+            mbar_init(smem_u32(&bars.v_full[i]), rank == 0 ? 4 + 1 : 4);
             mbar_init(smem_u32(&bars.s_full[i]), 1);
             mbar_init(smem_u32(&bars.pv_done[i]), 1);
         }
@@ -322,7 +319,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
 #pragma unroll 1
                 for (int j = 0; j < nt; ++j, ++t) {
                     const uint32_t slot = t % kFeedRing;
-                    mbar_wait_cluster(smem_u32(&bars.kv_full[slot]), (t / kFeedRing) & 1, wait_state, kTwK);
+                    mbar_wait_cluster(smem_u32(&bars.k_full[slot]), (t / kFeedRing) & 1, wait_state, kTwK);
                     if (t >= 2) wait(bars.s_read[t & 1], ((t >> 1) - 1) & 1, kTwSRead);
                     tc_fence_after_sync();
                     mma_ss_batch<D / 16>(tmem_base + (t & 1) * kTile, q_lo, desc_lo(smem_base + L::kK + slot * L::kKBytes, 16),
@@ -330,27 +327,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                     mma_commit_pair(smem_u32(&bars.s_full[slot]));
                 }
                 mma_commit_pair(smem_u32(&bars.q_free));
-            }
-        } else if (warp == 12) {
-            // ------------------------------------------------------------- hand-over: tells the first CTA what the second's feeder has written
-            // (An arrival that releases this CTA's writes to the other one takes 650 cycles of the warp that makes it; two of them a tile in
-            // the feeder were half of its time.)
-            const uint32_t q_bar = map_to_cta(smem_u32(&bars.q_full), 0);
-            uint32_t t = 0;
-#pragma unroll 1
-            for (int k = 0; same_in_warp(item_ready(k)); ++k) {
-                const int nt = same_in_warp(s_items[k % kTileItems].nt);
-                __syncwarp();
-                if (lane == 0) item_release(k);
-                wait(bars.q_full, k & 1, kTwQ);
-                __syncwarp();
-                if (lane == 0) mbar_arrive_release_cluster(q_bar);
-#pragma unroll 1
-                for (int j = 0; j < nt; ++j, ++t) {
-                    wait(bars.kv_full[t % kFeedRing], (t / kFeedRing) & 1, kTwK);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_release_cluster(map_to_cta(smem_u32(&bars.kv_full[t % kFeedRing]), 0));
-                }
             }
         } else if (rank == 0 && warp == 14) {
             // ------------------------------------------------------------- O += P V of the pair
@@ -368,12 +344,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                     const uint32_t slot = t % kFeedRing;
                     const uint32_t v_lo = desc_lo(smem_base + L::kV + slot * L::kVBytes, 0);
                     const uint32_t a_tmem = tmem_base + kTileTmemP + (t & 1) * (kTile / 2);
-                    mbar_wait_cluster(smem_u32(&bars.kv_full[slot]), (t / kFeedRing) & 1, wait_state, kTwV);
+                    mbar_wait_cluster(smem_u32(&bars.v_full[slot]), (t / kFeedRing) & 1, wait_state, kTwV);
                     wait(bars.p_full[t & 1], (t >> 1) & 1, kTwP);
                     tc_fence_after_sync();
 #pragma unroll 1
                     for (int ks = 0; ks < kTile / 16; ++ks) mma_ts_step<D>(d_tmem, a_tmem + ks * 8, v_lo + ks * kVDescStep<D>, kIdescPv, j + ks);
                     mma_commit_pair(smem_u32(&bars.pv_done[slot]));
+                }
+            }
+        } else if (warp == 12 || warp == 14) {
+            // ------------------------------------------------------------- hand-over: tells the first CTA what the second's feeder has written,
+            // warp 12 of Q and K, warp 14 of V.  (An arrival that releases this CTA's writes to the other one takes 650 cycles of the warp that
+            // makes it; two of them a tile in the feeder were half of its time.)
+            const uint64_t* const full = warp == 12 ? bars.k_full : bars.v_full;
+            uint32_t t = 0;
+#pragma unroll 1
+            for (int k = 0; same_in_warp(item_ready(k)); ++k) {
+                const int nt = same_in_warp(s_items[k % kTileItems].nt);
+                __syncwarp();
+                if (lane == 0) item_release(k);
+                if (warp == 12) {
+                    wait(bars.q_full, k & 1, kTwQ);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_release_cluster(map_to_cta(smem_u32(&bars.q_full), 0));
+                }
+#pragma unroll 1
+                for (int j = 0; j < nt; ++j, ++t) {
+                    wait(full[t % kFeedRing], (t / kFeedRing) & 1, warp == 12 ? kTwK : kTwV);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_release_cluster(map_to_cta(smem_u32(&full[t % kFeedRing]), 0));
                 }
             }
         }
@@ -386,22 +385,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
         const int row = tid & 127;
         const uint32_t tO = tmem_base + kTileTmemO + (static_cast<uint32_t>(fw * 32) << 16);
         const uint32_t o_free_bar = map_to_cta(smem_u32(&bars.o_free), 0);
-        uint32_t t = 0;
-        struct Finished {
-            int row0, n, head, chunk, whole, second, k;
-            uint32_t t_end;
-        } done{0, 0, 0, 0, 0, 0, -1, 0};
+        uint32_t t = 0, v = 0;              // tiles whose K, whose V has been fed
+        int started = 0, out_k = 0;         // items whose tiles are being fed or have been; the oldest that is not written out,
+        uint32_t out_end = 0;               // and the tiles up to its end
 
-        auto epilogue = [&]() {
+        // Writes item k out, its PVs being complete once its last tile's, t_end - 1, is.
+        auto epilogue = [&](int k, uint32_t t_end) {
+            const TileItem& done = s_items[k % kTileItems];
             const int rr = done.chunk * L::kRows + static_cast<int>(rank) * kTile + row;
             const bool row_ok = rr < done.n * p.G;
-            const float scale = s_scale[done.k & 3][row];
-            wait_asleep(bars.sums_full[done.k % kTileSums], (done.k / kTileSums) & 1, kTwSum);
-            const float2 sa = s_sums[done.k % kTileSums][0][row], sb = s_sums[done.k % kTileSums][1][row];
+            const float scale = s_scale[k & 3][row];
+            wait_asleep(bars.sums_full[k % kTileSums], (k / kTileSums) & 1, kTwSum);
+            const float2 sa = s_sums[k % kTileSums][0][row], sb = s_sums[k % kTileSums][1][row];
             const float m = fmaxf(sa.y, sb.y);
             const float l = m == -INFINITY ? 0.f : sa.x * fast_exp2((sa.y - m) * scale) + sb.x * fast_exp2((sb.y - m) * scale);
             const float inv = !done.whole ? 1.f : l > 0.f ? 1.f / l : 0.f;
-            wait_pv_done(done.t_end - 1, kTwODone);
+            wait_pv_done(t_end - 1, kTwODone);
             tc_fence_after_sync();
             const PackedRow at = packed_row(p, done.row0, done.head, row_ok ? rr : 0, D);
             float* const share = p.part + (2 * static_cast<int64_t>(blockIdx.x >> 1) + done.second) * L::kShareFloats;
@@ -438,13 +437,124 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                     p.lse[at.lse] = l > 0.f ? (m_log2 + log2f(l)) * 0.693147180559945309f : -INFINITY;
                 }
             }
+            __syncwarp();
+            if (lane == 0) item_release(k);
+        };
+
+        // Codes of a tile in registers: K's of keys g and g + 8 of this warp's 16 (heads of 64: two words of each are used), V's of keys k8 and
+        // k8 + 8 of two parts of 16, and their scales.  V's scales are 0 for keys behind the end or not there, whose bytes may be anything.
+        struct VCodes {
+            uint2 c[2][2];
+            uint32_t s[2];
+        };
+        uint4 kc[2];
+        uint32_t ks = 0;
+        unsigned there = 0;
+        VCodes v_now, v_one, v_two;  // of the tile just loaded, and of the one and two before
+        auto load = [&](int keys) {  // keys: of the tile, that there are
+            const uint32_t place = t % kRawRing;
+            wait(bars.raw_full[place], (t / kRawRing) & 1, kTwRaw);
+            there = s_raw_there[place];
+            const uint32_t raw = smem_base + L::kRaw + place * L::kRawBytes;
+            const uint32_t sub = raw + (4 * rank + fw) * L::kSubBytes;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (D == 128) kc[h] = ld_shared<uint4>(sub + h * 512 + lane * 16);
+                else *reinterpret_cast<uint2*>(&kc[h]) = ld_shared<uint2>(sub + h * 256 + lane * 8);
+            }
+            ks = D == 128 ? ld_shared<uint32_t>(sub + 16 * D + lane * 4) : ld_shared<uint32_t>(sub + 16 * D + (lane >> 1) * 4) >> (lane & 1) * 16;
+#pragma unroll
+            for (int s2 = 0; s2 < 2; ++s2) {
+                const uint32_t from = raw + (2 * fw + s2) * L::kSubBytes;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (D == 128) v_now.c[s2][h] = ld_shared<uint2>(from + 8 * D + ((h * 8 + eighth) * 8 + k8) * 8);
+                    else v_now.c[s2][h].x = ld_shared<uint32_t>(from + 8 * D + ((h * 8 + eighth) * 8 + k8) * 4);
+                }
+                v_now.s[s2] = ld_shared<uint32_t>(from + 17 * D + (D == 128 ? eighth : eighth >> 1) * 16 + (k8 >> 1) * 4);
+            }
+            if (keys < kTile || there != 0xffu) {
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if ((2 * fw + s2) * 16 + h * 8 + k8 >= keys || !(there >> (2 * fw + s2) & 1)) v_now.s[s2] &= h ? 0x0000ffffu : 0xffff0000u;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars.raw_free[place]));
+        };
+        // where this thread's chunks of 16 bytes go: eight lanes that store together hit all banks (of K's words the upper quarters of the head
+        // take theirs in another order)
+        const bool upper = D == 128 && c4 >= 2;
+        const uint32_t k_to = smem_base + L::kK + (upper ? L::kKPanelBytes : 0) + (fw * 16 + g) * 128;
+        const uint32_t k_chunk = D == 128 ? (4 * (c4 & 1)) ^ (upper ? 2 : 0) ^ g : (2 * c4) ^ g;
+        const uint32_t v_to = smem_base + L::kV + (fw * 32 + k8) * (D == 128 ? 128 : 64);
+        const uint32_t v_scale = k8 & 1 ? 0x11 : 0x00;  // byte of the word, twice
+        const uint32_t v_chunk = D == 128 ? (2 * e4) ^ k8 : e4 ^ (k8 >> 1);
+        // K of tile t, from the registers
+        auto feed_k = [&]() {
+            const uint32_t slot = t % kFeedRing, k_at = k_to + slot * L::kKBytes;
+            if (t >= kFeedRing) wait_s_full(t - kFeedRing, kTwKFree);
+            if (D == 128) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t two = scale_pair(ks >> (16 * h)), s0 = __byte_perm(two, 0, upper ? 0x3232 : 0x1010), s1 = __byte_perm(two, 0, upper ? 0x1010 : 0x3232);
+                    st_shared_values(k_at + h * 1024 + ((k_chunk ^ 0) << 4), upper ? kc[h].z : kc[h].x, s0);
+                    st_shared_values(k_at + h * 1024 + ((k_chunk ^ 1) << 4), upper ? kc[h].w : kc[h].y, s0);
+                    st_shared_values(k_at + h * 1024 + ((k_chunk ^ 2) << 4), upper ? kc[h].x : kc[h].z, s1);
+                    st_shared_values(k_at + h * 1024 + ((k_chunk ^ 3) << 4), upper ? kc[h].y : kc[h].w, s1);
+                }
+            } else {
+                const uint32_t two = scale_pair(ks);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t s0 = __byte_perm(two, 0, h ? 0x3232 : 0x1010);
+                    st_shared_values(k_at + h * 1024 + ((k_chunk ^ 0) << 4), kc[h].x, s0);
+                    st_shared_values(k_at + h * 1024 + ((k_chunk ^ 1) << 4), kc[h].y, s0);
+                }
+            }
+            if (warp == 8 && lane == 0) s_there[t % kFedRing] = there;
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&bars.k_full[slot]));
+                mbar_arrive(smem_u32(&bars.fed[t % kFedRing]));
+            }
+            ++t;
+        };
+        // V of tile v, from registers, and whatever is complete with it
+        auto feed_v = [&](const VCodes& x) {
+            const uint32_t slot = v % kFeedRing, v_at = v_to + slot * L::kVBytes;
+            if (v >= kFeedRing) wait_pv_done(v - kFeedRing, kTwVFree);
+#pragma unroll
+            for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t sc = scale_pair(__byte_perm(x.s[s2], 0, h ? v_scale + 0x22 : v_scale));
+                    const uint32_t at = v_at + (s2 * 16 + h * 8) * (D == 128 ? 128 : 64);
+                    st_shared_values(at + (v_chunk << 4), x.c[s2][h].x, sc);
+                    if (D == 128) st_shared_values(at + ((v_chunk ^ 1) << 4), x.c[s2][h].y, sc);
+                }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars.v_full[slot]));
+            ++v;
+        };
+        // An item is written out one tile behind its last V: that PV may be a tile or two away, and the tiles of the next one go on meanwhile.
+        // (No later: the PVs after that wait for the accumulator, and a fourth item for this one's place.)
+        auto write_out = [&](uint32_t behind) {
+            while (out_k < started && v >= out_end + behind) {
+                epilogue(out_k, out_end);
+                if (++out_k < started) out_end += s_items[out_k % kTileItems].nt;
+            }
         };
 
 #pragma unroll 1
         for (int k = 0; same_in_warp(item_ready(k)); ++k) {
-            const TileItem it = s_items[k % kTileItems];
-            __syncwarp();
-            if (lane == 0) item_release(k);
+            const TileItem& it = s_items[k % kTileItems];
+            const int nt = it.nt, t0 = it.t0, ns = it.ns, skip = it.skip, len = it.len;
+            if (out_k == k) out_end = t + nt;
+            started = k + 1;
             // ---- Q: a row a thread, scaled by a power of two to at most 2
             if (k > 0) wait(bars.q_free, (k - 1) & 1, kTwQFree);
             {
@@ -480,103 +590,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars.q_full));
-            // ---- the tiles.  A tile's codes are in registers before the tile before it is handed on, so that neither the fetch nor
-            // shared memory's latency stand between two tiles, and its place in the ring of packed tiles is free as soon as they are.
-            uint4 kc[2];            // K: codes of keys g and g + 8 of this warp's 16 (heads of 64: two words of each are used)
-            uint32_t ks = 0;        // and their scales
-            uint2 vc[2][2];         // V: codes of keys k8 and k8 + 8 of two parts of 16 keys
-            uint32_t vs[2][2];      // and their scale
-            unsigned there = 0;
-            auto load = [&](uint32_t u) {
-                const uint32_t place = u % kRawRing;
-                wait(bars.raw_full[place], (u / kRawRing) & 1, kTwRaw);
-                there = s_raw_there[place];
-                const uint32_t raw = smem_base + L::kRaw + place * L::kRawBytes;
-                const uint32_t sub = raw + (4 * rank + fw) * L::kSubBytes;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (D == 128) kc[h] = ld_shared<uint4>(sub + h * 512 + lane * 16);
-                    else *reinterpret_cast<uint2*>(&kc[h]) = ld_shared<uint2>(sub + h * 256 + lane * 8);
-                }
-                ks = D == 128 ? ld_shared<uint32_t>(sub + 16 * D + lane * 4) : ld_shared<uint32_t>(sub + 16 * D + (lane >> 1) * 4) >> (lane & 1) * 16;
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t v = raw + (2 * fw + s2) * L::kSubBytes;
-                        if (D == 128) vc[s2][h] = ld_shared<uint2>(v + 8 * D + ((h * 8 + eighth) * 8 + k8) * 8);
-                        else vc[s2][h].x = ld_shared<uint32_t>(v + 8 * D + ((h * 8 + eighth) * 8 + k8) * 4);
-                        vs[s2][h] = ld_shared_u8(v + 17 * D + (D == 128 ? eighth : eighth >> 1) * 16 + (k8 >> 1) * 4 + h * 2 + (k8 & 1));
-                    }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars.raw_free[place]));
-            };
-            // where this thread's chunks of 16 bytes go: eight lanes that store together hit all banks (of K's words the upper quarters of the head
-            // take theirs in another order)
-            const bool upper = D == 128 && c4 >= 2;
-            const uint32_t k_to = smem_base + L::kK + (upper ? L::kKPanelBytes : 0) + (fw * 16 + g) * 128;
-            const uint32_t k_chunk = D == 128 ? (4 * (c4 & 1)) ^ (upper ? 2 : 0) ^ g : (2 * c4) ^ g;
-            const uint32_t v_to = smem_base + L::kV + (fw * 32 + k8) * (D == 128 ? 128 : 64);
-            const uint32_t v_chunk = D == 128 ? (2 * e4) ^ k8 : e4 ^ (k8 >> 1);
-            load(t);
 #pragma unroll 1
-            for (int j = 0; j < it.nt; ++j, ++t) {
-                const uint32_t slot = t % kFeedRing;
-                if (t >= kFeedRing) {
-                    wait_s_full(t - kFeedRing, kTwKFree);
-                    wait_pv_done(t - kFeedRing, kTwVFree);
-                }
-                // ---- K: 16 keys a warp, those of this CTA
-                const uint32_t k_at = k_to + slot * L::kKBytes;
-                if (D == 128) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t two = scale_pair(ks >> (16 * h)), s0 = __byte_perm(two, 0, upper ? 0x3232 : 0x1010), s1 = __byte_perm(two, 0, upper ? 0x1010 : 0x3232);
-                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 0) << 4), upper ? kc[h].z : kc[h].x, s0);
-                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 1) << 4), upper ? kc[h].w : kc[h].y, s0);
-                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 2) << 4), upper ? kc[h].x : kc[h].z, s1);
-                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 3) << 4), upper ? kc[h].y : kc[h].w, s1);
-                    }
-                } else {
-                    const uint32_t two = scale_pair(ks);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t s0 = __byte_perm(two, 0, h ? 0x3232 : 0x1010);
-                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 0) << 4), kc[h].x, s0);
-                        st_shared_values(k_at + h * 1024 + ((k_chunk ^ 1) << 4), kc[h].y, s0);
-                    }
-                }
-                // ---- V: 32 keys a warp, this CTA's columns; zeros for keys behind the end or not there, whose bytes may be anything
-                const int key0 = ((it.t0 + j < it.ns) ? it.t0 + j : it.t0 + j + it.skip) << 7;
-                const uint32_t v_at = v_to + slot * L::kVBytes;
-                const bool clean = key0 + kTile <= it.len && there == 0xffu;
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t s = scale_pair(vs[s2][h] | vs[s2][h] << 8);
-                        if (!clean && (key0 + (2 * fw + s2) * 16 + h * 8 + k8 >= it.len || !(there >> (2 * fw + s2) & 1))) s = 0u;
-                        const uint32_t at = v_at + (s2 * 16 + h * 8) * (D == 128 ? 128 : 64);
-                        st_shared_values(at + (v_chunk << 4), vc[s2][h].x, s);
-                        if (D == 128) st_shared_values(at + ((v_chunk ^ 1) << 4), vc[s2][h].y, s);
-                    }
-                if (warp == 8 && lane == 0) s_there[t % kFedRing] = there;
-                if (j + 1 < it.nt) load(t + 1);
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(smem_u32(&bars.fed[t % kFedRing]));
-                    mbar_arrive(smem_u32(&bars.kv_full[slot]));
-                }
-                // the item before is written out once this one's first tiles are on their way (no later: their PV needs the accumulator)
-                if (done.k >= 0 && j == min(1, it.nt - 1)) {
-                    epilogue();
-                    done.k = -1;
-                }
+            for (int j = t0; j < t0 + nt; ++j) {
+                load(len - ((j < ns ? j : j + skip) << 7));
+                feed_k();
+                if (t > 2) feed_v(v_two);
+                v_two = v_one;
+                v_one = v_now;
+                write_out(1);
             }
-            done = {it.row0, it.n, it.head, it.chunk, it.whole, it.second, k, t};
         }
-        if (done.k >= 0) epilogue();
+        if (t > 1) feed_v(v_two);
+        if (t > 0) feed_v(v_one);
+        write_out(0);
     } else {
         // ----------------------------------------------------------------- softmax, every other key tile
         reg_alloc<184>();
