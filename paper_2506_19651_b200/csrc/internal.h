@@ -255,8 +255,7 @@ struct PackedAttnParams {
     Divisor div_g;
     float scale_log2;        // softmax scale * log2(e)
 };
-// `rows`: most rows of one sequence and kv head.  Up to kPackedFewRows of them go to packed_attn_kernel, more to packed_tile_kernel.
-constexpr int kPackedFewRows = 32;
+// `rows`: most rows of one sequence and kv head; few of them go to packed_attn_kernel, more to packed_tile_kernel.
 size_t packed_attn_workspace_bytes(int head_dim, int64_t rows);
 cudaError_t launch_packed_attn(const PackedAttnParams& p, int head_dim, int64_t rows, cudaStream_t stream);
 cudaError_t launch_packed_tile(const PackedAttnParams& p, int head_dim, cudaStream_t stream);  // without its merge

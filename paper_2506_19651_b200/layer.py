@@ -205,3 +205,79 @@ class StreamingWindow:
                           self.S + self.blocks_seen * self.B, Qn)
         pb.pevlm_query_attn(s, self.q_buf, self.k_cache, self.v_cache, o, lse, self.ws_query)
         return o, lse
+
+
+class PackedCache:
+    """Keys and values of one layer of many sequences, in pages and in 4 bits: what a server keeps of its videos between questions
+    (a 74K-token video of 4 kv heads of 128: 42.6 MB a layer instead of 151.5).  Lengths, page tables, slots and positions live on the
+    GPU, so a step may be captured into a graph and replayed with whatever `new_lens` and `finished` hold by then.
+
+    `max_rows` rows at most a step, of all sequences one after another; `window` > 0 leaves each row the last `window` positions and its
+    sequence's first `sink` ones.  A sequence that finds no pages keeps its length and its rows get slot -1 (see pevlm_pages_assign)."""
+
+    def __init__(self, num_seqs, max_tokens, num_pages, page_len, max_rows, Hq, Hkv, d, theta, window=0, sink=0, scale=0.0, device="cuda"):
+        import torch
+        if max_rows < 1:
+            raise ValueError(f"a step of {max_rows} rows")
+        self.pages = pb.make_pages(num_pages, page_len, num_seqs, -(-max_tokens // page_len))
+        self.shape = pb.make_shape(sink, 1, 0, 1, Hq, Hkv, d, theta=theta, scale=scale)
+        n_bytes = pb.pevlm_packed_cache_bytes(self.shape, self.pages)
+        if n_bytes == 0:
+            raise ValueError(f"no packed cache of {num_pages} pages of {page_len} tokens for {num_seqs} sequences of {max_tokens}, {Hq}/{Hkv} heads of {d}")
+        self.Hq, self.Hkv, self.d, self.window, self.max_rows = Hq, Hkv, d, window, max_rows
+        ints = lambda n: torch.zeros(n, dtype=torch.int32, device=device)
+        self.cache = torch.zeros(n_bytes, dtype=torch.uint8, device=device)
+        self.page_table = torch.full((num_seqs, self.pages.max_pages), -1, dtype=torch.int32, device=device)
+        self.free_list = torch.arange(num_pages, dtype=torch.int32, device=device)
+        self.lens, self._lens = ints(num_seqs), ints(num_seqs)  # after a step; between its two calls
+        self.free_count, self._free_count = torch.full((1,), num_pages, dtype=torch.int32, device=device), ints(1)
+        self.row_start, self.slots, self.positions = ints(num_seqs + 1), ints(max_rows), ints(max_rows)
+        self._none = ints(num_seqs)
+        self._q, self._k = (torch.empty((max_rows, h, d), dtype=torch.bfloat16, device=device) for h in (Hq, Hkv))
+        self._lse = torch.empty(0, dtype=torch.float32, device=device)
+        self.workspace = torch.zeros(pb.pevlm_packed_workspace_bytes(self.shape, self.pages, max_rows, max_rows), dtype=torch.uint8, device=device)
+
+    def _rows(self, *tensors):
+        n = tensors[0].shape[0]
+        if n > self.max_rows or any(t.shape[0] != n for t in tensors):
+            raise ValueError(f"{', '.join(str(t.shape[0]) for t in tensors)} rows where at most {self.max_rows} fit, the same of each")
+        return n
+
+    def extend(self, new_lens, finished=None):
+        """Gives back the pages of the `finished` sequences and makes room for new_lens (int32, on the GPU, one for each sequence) more tokens
+        of each: row_start, slots and positions say where the rows of the step go."""
+        if new_lens.numel() != self.pages.num_seqs or (finished is not None and finished.numel() != self.pages.num_seqs):
+            raise ValueError(f"lengths of {self.pages.num_seqs} sequences")
+        pb.pevlm_pages_release(self.pages, self._none if finished is None else finished, self.lens, self.page_table, self.free_list,
+                               self.free_count, self._lens, self._free_count)
+        pb.pevlm_pages_assign(self.pages, self._lens, new_lens, self.page_table, self.free_list, self._free_count, self.lens,
+                              self.free_count, self.row_start, self.slots, self.positions, self.max_rows)
+
+    def store(self, k, v):
+        """Rows of roped K and of V [n, Hkv, d] (rows may be strided) into the slots of the last extend()."""
+        n = self._rows(k, v)
+        pb.pevlm_packed_store(self.shape, self.pages, k, v, self.slots, n, self.cache, k.stride(0), v.stride(0))
+
+    def attend(self, q, most=None):
+        """Attention of roped q [n, Hq, d], the rows of the last extend().  `most`: rows of one sequence, if the caller knows.
+        Returns (o [n,Hq,d], lse [Hq,n])."""
+        n = self._rows(q)
+        o, lse = q.new_empty((n, self.Hq, self.d)), self._lse.new_empty((self.Hq, n))
+        pb.pevlm_packed_attn(self.shape, self.pages, self.window, q, self.cache, self.page_table, self.lens, self.row_start, n,
+                             n if most is None else min(most, n), o, lse, self.workspace, q.stride(0))
+        return o, lse
+
+    def step(self, q, k, v, new_lens, finished=None, most=None):
+        """One step of the layer from un-roped rows: extend(), RoPE at the rows' positions, store(), attend()."""
+        n = self._rows(q, k, v)
+        self.extend(new_lens, finished)
+        pb.pevlm_rope_qk(self.shape, q, k, self._q, self._k, 0, n, self.positions)
+        self.store(self._k[:n], v)
+        return self.attend(self._q[:n], most)
+
+    def load(self, slots):
+        """K and V [n, Hkv, d] (bf16) as the cache holds them at the given slots (int32, on the GPU)."""
+        n = slots.numel()
+        k, v = (self._k.new_empty((n, self.Hkv, self.d)) for _ in range(2))
+        pb.pevlm_packed_load(self.shape, self.pages, self.cache, slots, n, k, v)
+        return k, v

@@ -166,3 +166,26 @@ def test_window_attn(lib):
     assert attn(n=0, q=None, k=None, v=None, o=None) == pb.PEVLM_OK
     # one workspace for any cache and window of the same rows
     assert pb.pevlm_window_workspace_bytes(s, 1, 0, 4) == size == pb.pevlm_window_workspace_bytes(s, 2 ** 31 - 1, 10 ** 6, 4)
+
+
+def test_packed_cache_refuses(monkeypatch):
+    import torch
+    from paper_2506_19651_b200 import layer
+    pbuild.build()
+    monkeypatch.setattr(pb, "_native", lambda: pytest.fail("a call was made"))
+    with pytest.raises(ValueError, match="no packed cache"):
+        layer.PackedCache(2, 100, 4, 24, 8, 4, 2, 64, 1e4, device="cpu")
+    with pytest.raises(ValueError, match="step of 0 rows"):
+        layer.PackedCache(2, 100, 4, 16, 0, 4, 2, 64, 1e4, device="cpu")
+    c = layer.PackedCache(2, 100, 14, 16, 8, 4, 2, 64, 1e4, device="cpu")
+    rows = lambda n: [torch.zeros(n, h, 64, dtype=torch.bfloat16) for h in (4, 2, 2)]
+    lens = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="at most 8 fit"):
+        c.step(*rows(9), lens)
+    q, k, v = rows(4)
+    with pytest.raises(ValueError, match="the same of each"):
+        c.step(q, k[:3], v, lens)
+    with pytest.raises(ValueError, match="2 sequences"):
+        c.step(q, k, v, torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="2 sequences"):
+        c.extend(lens, torch.zeros(1, dtype=torch.int32))
