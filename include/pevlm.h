@@ -18,7 +18,7 @@
  *   - All tensor pointers are DEVICE pointers, contiguous, bf16 (2-byte brain float) unless
  *     stated, and 16-byte aligned; the attention OUTPUT `o` of pevlm_parallel_prefill_attn,
  *     pevlm_block_attn and pevlm_query_attn(_noalloc) must be 32-byte aligned (its rows are
- *     written with 32-byte vector stores), workspaces 256-byte aligned.  A pointer that misses
+ *     written with 32-byte vector stores; likewise those of the calls below that say so), workspaces 256-byte aligned.  A pointer that misses
  *     its alignment is refused with PEVLM_EALIGN before any launch.  `stream` is a
  *     cudaStream_t passed as void* (NULL = the legacy default stream).  `shape` is a HOST
  *     pointer.  Input values must be finite.
@@ -220,7 +220,7 @@ int pevlm_layer_forward(const pevlm_shape_t* shape, int32_t last_len, const void
  * counts) or j < sink_len (of shape).  One call serves a whole prefill (first_token = 0), a chunk of one behind a cache, and single
  * tokens (few rows take a kernel of their own, like those of pevlm_query_attn).
  *   q [n_tokens, Hq, d] roped; k_cache, v_cache [cache_rows, Hkv, d], of which rows [0, first_token + n_tokens) may be read
- *   (cache_rows >= that); o [n_tokens, Hq, d], lse [Hq, n_tokens] (may be NULL)
+ *   (cache_rows >= that); o [n_tokens, Hq, d] (32-byte aligned), lse [Hq, n_tokens] (may be NULL)
  * batch > 1: sequences of equal lengths, n_tokens rows of q and o, cache_rows rows of the caches apart.  Of `shape` batch, sink_len, the head
  * counts, head_dim and softmax_scale are used.  window >= 1; first_token + n_tokens <= 2^30.
  * workspace: >= pevlm_window_workspace_bytes(...) bytes, 256-byte aligned; that of a call does for any first_token and window.
@@ -303,7 +303,7 @@ size_t pevlm_packed_cache_bytes(const pevlm_shape_t* shape, const pevlm_pages_t*
 int pevlm_packed_store(const pevlm_shape_t* shape, const pevlm_pages_t* pages, const void* k, const void* v, int64_t k_stride,
                        int64_t v_stride, const int32_t* slots, int64_t n_rows, void* cache, void* stream);
 
-/* Reads rows back: k_out, v_out [n_rows, Hkv, d] bf16 receive what the cache holds at slots [n_rows] (any order, any of them more than
+/* Reads rows back: k_out, v_out [n_rows, Hkv, d] bf16, 32-byte aligned, receive what the cache holds at slots [n_rows] (any order, any of them more than
  * once); zeros for a slot out of range. */
 int pevlm_packed_load(const pevlm_shape_t* shape, const pevlm_pages_t* pages, const void* cache, const int32_t* slots, int64_t n_rows,
                       void* k_out, void* v_out, void* stream);

@@ -229,6 +229,7 @@ struct PackedRows {
     int64_t k_stride, v_stride;  // elements from row to row
     int64_t n_rows;
     int32_t Hkv, n_slots, page_shift;
+    Divisor div_heads;  // by 2 * Hkv (set by the launch)
 };
 cudaError_t launch_packed_store(const PackedRows& p, int head_dim, cudaStream_t stream);
 cudaError_t launch_packed_load(const PackedRows& p, int head_dim, cudaStream_t stream);

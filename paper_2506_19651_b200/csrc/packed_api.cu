@@ -5,6 +5,11 @@
 
 namespace pevlm {
 
+// Rows of one call: its blocks (64 rows of a head at most, see packed_kernel.cu) have to be counted in 31 bits.
+static bool countable_rows(const pevlm_shape_t* s, int64_t n_rows) {
+    return n_rows <= 1ll << 30 && (n_rows + 255) / 64 * 2 * s->num_kv_heads < 1ll << 31;
+}
+
 static int check_pages(const pevlm_pages_t* g) {
     if (!g || g->num_pages < 1 || g->num_seqs < 1 || g->max_pages < 1) return PEVLM_EINVAL;
     if (g->page_len != 16 && g->page_len != 32 && g->page_len != 64 && g->page_len != 128) return PEVLM_EUNSUPPORTED;
@@ -20,7 +25,7 @@ static int check_packed(const pevlm_shape_t* s, const pevlm_pages_t* g) {
     int rc = check_shape(s);
     if (rc == PEVLM_OK) rc = check_pages(g);
     if (rc != PEVLM_OK) return rc;
-    return s->batch == 1 && s->num_kv_heads <= 32767 ? PEVLM_OK : PEVLM_EUNSUPPORTED;  // kv heads: a dimension of the grids
+    return s->batch == 1 ? PEVLM_OK : PEVLM_EUNSUPPORTED;
 }
 
 }  // namespace pevlm
@@ -75,7 +80,7 @@ int pevlm_packed_store(const pevlm_shape_t* s, const pevlm_pages_t* g, const voi
                        int64_t v_stride, const int32_t* slots, int64_t n_rows, void* cache, void* stream) {
     int rc = check_packed(s, g);
     if (rc != PEVLM_OK) return rc;
-    if (n_rows < 0 || n_rows > 1ll << 30) return PEVLM_EINVAL;
+    if (n_rows < 0 || !countable_rows(s, n_rows)) return PEVLM_EINVAL;
     if (!cache || (n_rows > 0 && (!k || !v || !slots))) return PEVLM_EINVAL;
     const int64_t row = static_cast<int64_t>(s->num_kv_heads) * s->head_dim;
     if (k_stride == 0) k_stride = row;
@@ -102,9 +107,9 @@ int pevlm_packed_load(const pevlm_shape_t* s, const pevlm_pages_t* g, const void
                       void* k_out, void* v_out, void* stream) {
     int rc = check_packed(s, g);
     if (rc != PEVLM_OK) return rc;
-    if (n_rows < 0 || n_rows > 1ll << 30) return PEVLM_EINVAL;
+    if (n_rows < 0 || !countable_rows(s, n_rows)) return PEVLM_EINVAL;
     if (!cache || (n_rows > 0 && (!k_out || !v_out || !slots))) return PEVLM_EINVAL;
-    if (!aligned_to(k_out, 16) || !aligned_to(v_out, 16) || !aligned_to(cache, 16) || !aligned_to(slots, 4)) return PEVLM_EALIGN;
+    if (!aligned_to(k_out, 32) || !aligned_to(v_out, 32) || !aligned_to(cache, 16) || !aligned_to(slots, 4)) return PEVLM_EALIGN;
     if (n_rows == 0) return PEVLM_OK;
     rc = check_device();
     if (rc != PEVLM_OK) return rc;

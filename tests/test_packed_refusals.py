@@ -79,6 +79,8 @@ def test_packed_rows(lib):
             assert f(s, g, **{name: at(4098)}) == pb.PEVLM_EALIGN
         assert f(s, g, n=-1) == pb.PEVLM_EINVAL and f(s, g, n=2 ** 30 + 1) == pb.PEVLM_EINVAL
         assert f(s, g, n=0, k=None, v=None, sl=None) == pb.PEVLM_OK
+    assert load(s, g, k=at(4096 + 16)) == pb.PEVLM_EALIGN and load(s, g, v=at(4096 + 16)) == pb.PEVLM_EALIGN  # written 32 bytes at a time
+    assert store(s, g, k=at(4096 + 16), n=0) == pb.PEVLM_OK
     assert store(s, g, ks=120) == pb.PEVLM_EINVAL and store(s, g, vs=-128) == pb.PEVLM_EINVAL
     assert store(s, g, ks=132) == pb.PEVLM_EALIGN
 
