@@ -11,9 +11,7 @@
 
 namespace pevlm {
 
-constexpr int kPagesThreads = 1024;
-constexpr int kPagesWarps = kPagesThreads / 32;
-constexpr int kRowsPerCta = 4 * kPagesThreads;
+constexpr int kMostThreads = 1024;
 
 struct Sums {
     int64_t rows, pages;
@@ -24,8 +22,10 @@ __device__ __forceinline__ Sums shifted_up(const Sums& a, int by) {
 }
 
 // Inclusive sums over the CTA's threads; `all`: over all of them.
+template <int THREADS>
 __device__ __forceinline__ Sums scan(Sums x, Sums& all) {
-    __shared__ Sums of_warp[kPagesWarps];
+    constexpr int kWarps = THREADS / 32;
+    __shared__ Sums of_warp[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int by = 1; by < 32; by *= 2) {
@@ -34,14 +34,24 @@ __device__ __forceinline__ Sums scan(Sums x, Sums& all) {
     }
     if (lane == 31) of_warp[warp] = x;
     __syncthreads();
-    Sums w = of_warp[lane];
+    if (kWarps <= 4) {
+        Sums before{0, 0};
+        all = {0, 0};
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w == warp) before = all;
+            all = all + of_warp[w];
+        }
+        return x + before;
+    }
+    Sums w = of_warp[lane % kWarps];
 #pragma unroll
     for (int by = 1; by < 32; by *= 2) {
         const Sums y = shifted_up(w, by);
         if (lane >= by) w = w + y;
     }
     const Sums before{__shfl_sync(0xffffffffu, w.rows, max(warp - 1, 0)), __shfl_sync(0xffffffffu, w.pages, max(warp - 1, 0))};
-    all = {__shfl_sync(0xffffffffu, w.rows, 31), __shfl_sync(0xffffffffu, w.pages, 31)};
+    all = {__shfl_sync(0xffffffffu, w.rows, kWarps - 1), __shfl_sync(0xffffffffu, w.pages, kWarps - 1)};
     return warp > 0 ? x + before : x;
 }
 
@@ -58,8 +68,10 @@ __device__ __forceinline__ int last_at_or_before(const int* starts, int n, int x
 
 __device__ __forceinline__ int clamped(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
-__global__ void __launch_bounds__(kPagesThreads) assign_kernel(const __grid_constant__ AssignParams p) {
-    __shared__ int s_start[kPagesThreads], s_len[kPagesThreads], s_top[kPagesThreads];  // of the sequences of this turn
+// A thread has ROWS neighbouring rows at a time.
+template <int THREADS, int ROWS>
+__global__ void __launch_bounds__(THREADS) assign_kernel(const __grid_constant__ AssignParams p) {
+    __shared__ int s_start[THREADS], s_len[THREADS], s_top[THREADS];  // of the sequences of this turn
     grid_wait();
     grid_launch_dependents();
     const int tid = threadIdx.x, P = 1 << p.page_shift, capacity = p.max_pages << p.page_shift;
@@ -67,8 +79,8 @@ __global__ void __launch_bounds__(kPagesThreads) assign_kernel(const __grid_cons
     const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows_per_cta, row1 = min(row0 + p.rows_per_cta, p.max_rows);
     Sums base{0, 0};
     int64_t taken = 0;  // pages of the sequences that got theirs: what the last of them has as its inclusive sum
-    for (int r0 = 0; r0 < p.num_seqs; r0 += kPagesThreads) {
-        const int r = r0 + tid, n = min(kPagesThreads, p.num_seqs - r0);
+    for (int r0 = 0; r0 < p.num_seqs; r0 += THREADS) {
+        const int r = r0 + tid, n = min(THREADS, p.num_seqs - r0);
         const bool there = r < p.num_seqs;
         const int len = there ? clamped(p.lens[r], 0, capacity) : 0;
         const int add = there ? max(p.new_lens[r], 0) : 0;
@@ -76,7 +88,7 @@ __global__ void __launch_bounds__(kPagesThreads) assign_kernel(const __grid_cons
         const bool fits = static_cast<int64_t>(len) + add <= capacity;  // its row of the table
         const int need = fits ? ((len + add + P - 1) >> p.page_shift) - have : 0;
         Sums all;
-        const Sums to = base + scan(Sums{add, need}, all);
+        const Sums to = base + scan<THREADS>(Sums{add, need}, all);
         // Of those that fit their rows, the ones that get pages are all up to some sequence: behind the first that takes the sums past
         // max_rows or past the free list no later one with new rows (with fresh pages) stays within.  So no page is passed over.
         const bool granted = there && fits && to.rows <= p.max_rows && (need == 0 || to.pages <= count);
@@ -95,11 +107,11 @@ __global__ void __launch_bounds__(kPagesThreads) assign_kernel(const __grid_cons
             s_top[tid] = static_cast<int>(count - 1 - (to.pages - need) + have);
             __syncthreads();
             const int64_t lo = max(first, row0), hi = min(last, row1);
-            for (int64_t g = (lo & ~3ll) + 4 * tid; g < hi; g += 4 * kPagesThreads) {
+            for (int64_t g = lo / ROWS * ROWS + ROWS * tid; g < hi; g += ROWS * THREADS) {
                 int q = last_at_or_before(s_start, n, static_cast<int>(max(g, lo)));
-                int slot[4], position[4];
+                int slot[ROWS], position[ROWS], page = -1, page_q = -1, page_index = -1;  // neighbours mostly share a page
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < ROWS; ++i) {
                     const int64_t row = g + i;
                     slot[i] = -1;
                     position[i] = 0;
@@ -110,18 +122,22 @@ __global__ void __launch_bounds__(kPagesThreads) assign_kernel(const __grid_cons
                     position[i] = static_cast<int>(min(pos, static_cast<int64_t>(INT32_MAX)));
                     if (s_len[q] < 0) continue;
                     const int index = static_cast<int>(pos >> p.page_shift);
-                    int32_t* const entry = p.page_table + static_cast<int64_t>(r0 + q) * p.max_pages + index;
-                    const bool fresh = index >= (held + P - 1) >> p.page_shift;
-                    const int page = fresh ? p.free_list[s_top[q] - index] : *entry;
-                    if (fresh && (pos & (P - 1)) == 0) *entry = page;
+                    if (q != page_q || index != page_index) {
+                        int32_t* const entry = p.page_table + static_cast<int64_t>(r0 + q) * p.max_pages + index;
+                        const bool fresh = index >= (held + P - 1) >> p.page_shift;
+                        page = fresh ? p.free_list[s_top[q] - index] : *entry;
+                        page_q = q;
+                        page_index = index;
+                        if (fresh && (pos & (P - 1)) == 0) *entry = page;
+                    }
                     if (page >= 0 && page < p.num_pages) slot[i] = (page << p.page_shift) + static_cast<int>(pos & (P - 1));
                 }
-                if (g >= lo && g + 4 <= hi) {
-                    *reinterpret_cast<int4*>(p.slots + g) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-                    *reinterpret_cast<int4*>(p.positions + g) = make_int4(position[0], position[1], position[2], position[3]);
+                if (ROWS == 4 && g >= lo && g + 4 <= hi) {
+                    *reinterpret_cast<int4*>(p.slots + g) = make_int4(slot[0], slot[1 % ROWS], slot[2 % ROWS], slot[3 % ROWS]);
+                    *reinterpret_cast<int4*>(p.positions + g) = make_int4(position[0], position[1 % ROWS], position[2 % ROWS], position[3 % ROWS]);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < ROWS; ++i) {
                         if (g + i < lo || g + i >= hi) continue;
                         p.slots[g + i] = slot[i];
                         p.positions[g + i] = position[i];
@@ -133,7 +149,7 @@ __global__ void __launch_bounds__(kPagesThreads) assign_kernel(const __grid_cons
         __syncthreads();  // the arrays and the warps' sums are written again
     }
     // rows that no sequence has
-    for (int64_t row = max(base.rows, row0) + tid; row < row1; row += kPagesThreads) {
+    for (int64_t row = max(base.rows, row0) + tid; row < row1; row += THREADS) {
         p.slots[row] = -1;
         p.positions[row] = 0;
     }
@@ -150,27 +166,28 @@ __global__ void __launch_bounds__(kPagesThreads) assign_kernel(const __grid_cons
     }
 }
 
-__global__ void __launch_bounds__(kPagesThreads) release_kernel(const __grid_constant__ ReleaseParams p) {
-    __shared__ int s_start[kPagesThreads];
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) release_kernel(const __grid_constant__ ReleaseParams p) {
+    __shared__ int s_start[THREADS];
     grid_wait();
     grid_launch_dependents();
     const int tid = threadIdx.x, P = 1 << p.page_shift, capacity = p.max_pages << p.page_shift;
     const int64_t count = clamped(*p.free_count, 0, p.num_pages);
     Sums base{0, 0};
-    for (int r0 = 0; r0 < p.num_seqs; r0 += kPagesThreads) {
-        const int r = r0 + tid, n = min(kPagesThreads, p.num_seqs - r0);
+    for (int r0 = 0; r0 < p.num_seqs; r0 += THREADS) {
+        const int r = r0 + tid, n = min(THREADS, p.num_seqs - r0);
         const bool there = r < p.num_seqs;
         const int len = there ? clamped(p.lens[r], 0, capacity) : 0;
         const bool finished = there && p.finished[r] != 0;
         const int given = finished ? (len + P - 1) >> p.page_shift : 0;
         Sums all;
-        const Sums to = base + scan(Sums{0, given}, all);
+        const Sums to = base + scan<THREADS>(Sums{0, given}, all);
         if (blockIdx.x == 0 && there) p.lens_out[r] = finished ? 0 : len;
         if (all.pages > 0) {
             s_start[tid] = static_cast<int>(min(to.pages - given - base.pages, static_cast<int64_t>(INT32_MAX)));
             __syncthreads();
             const int64_t at = count + base.pages, room = min(all.pages, p.num_pages - at);
-            for (int64_t i = static_cast<int64_t>(blockIdx.x) * kPagesThreads + tid; i < room; i += static_cast<int64_t>(gridDim.x) * kPagesThreads) {
+            for (int64_t i = static_cast<int64_t>(blockIdx.x) * THREADS + tid; i < room; i += static_cast<int64_t>(gridDim.x) * THREADS) {
                 const int q = last_at_or_before(s_start, n, static_cast<int>(i));
                 p.free_list[at + i] = p.page_table[static_cast<int64_t>(r0 + q) * p.max_pages + (i - s_start[q])];
             }
@@ -181,16 +198,26 @@ __global__ void __launch_bounds__(kPagesThreads) release_kernel(const __grid_con
     if (blockIdx.x == 0 && tid == 0) *p.free_count_out = static_cast<int>(min(count + base.pages, static_cast<int64_t>(p.num_pages)));
 }
 
+// Few sequences and rows: CTAs of 128 threads, whose barriers and sums take less (64 sequences, one row each: both calls 4.5 us, 7.9 with 1,024 threads of four rows).
 cudaError_t launch_assign(AssignParams p, cudaStream_t stream) {
-    const int64_t want = (p.max_rows + kRowsPerCta - 1) / kRowsPerCta;
+    if (p.num_seqs <= 128 && p.max_rows <= 512) {
+        p.rows_per_cta = p.max_rows;
+        return launch_chained<assign_kernel<128, 1>>(dim3(1), 128, 0, stream, p);
+    }
+    const int64_t want = (p.max_rows + 4 * kMostThreads - 1) / (4 * kMostThreads);
     const unsigned grid = static_cast<unsigned>(want < 1 ? 1 : want > kNumSms ? kNumSms : want);
     p.rows_per_cta = ((p.max_rows + grid - 1) / grid + 3) & ~3ll;
-    return launch_chained<assign_kernel>(dim3(grid), kPagesThreads, 0, stream, p);
+    return launch_chained<assign_kernel<kMostThreads, 4>>(dim3(grid), kMostThreads, 0, stream, p);
 }
 
 cudaError_t launch_release(const ReleaseParams& p, cudaStream_t stream) {
-    const int64_t want = static_cast<int64_t>(p.num_seqs) * p.max_pages / (8 * kPagesThreads);
-    return launch_chained<release_kernel>(dim3(static_cast<unsigned>(want < 1 ? 1 : want > 32 ? 32 : want)), kPagesThreads, 0, stream, p);
+    const int64_t entries = static_cast<int64_t>(p.num_seqs) * p.max_pages;
+    if (p.num_seqs <= 128) {
+        const int64_t want = entries / 1024;
+        return launch_chained<release_kernel<128>>(dim3(static_cast<unsigned>(want < 1 ? 1 : want > 16 ? 16 : want)), 128, 0, stream, p);
+    }
+    const int64_t want = entries / (8 * kMostThreads);
+    return launch_chained<release_kernel<kMostThreads>>(dim3(static_cast<unsigned>(want < 1 ? 1 : want > 32 ? 32 : want)), kMostThreads, 0, stream, p);
 }
 
 }  // namespace pevlm
