@@ -681,6 +681,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
                 tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(s_read_bar);
+                unsigned live = 0xfu;  // sliding window: parts of 32 columns of which the warp's rows see anything
                 if (need_mask) {
                     // by 32 columns: on the diagonal the rows of a warp differ within one such part only, the others are
                     // visible or hidden as a whole (a compare for each of the 128 columns took 1,200 cycles a tile)
@@ -688,6 +689,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
                     for (int c = 0; c < 4; ++c) {
                         const int cols = max_col - c * 32;  // visible ones of this part
                         if (__all_sync(0xffffffffu, cols >= 32)) continue;
+                        if ((MODE & 4) && __all_sync(0xffffffffu, cols <= 0)) live &= ~(1u << c);
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (i >= cols) r[c * 32 + i] = 0xff800000u;  // -inf
@@ -700,6 +702,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
                         for (int c = 0; c < 4; ++c) {
                             const int from = band - key0 - c * 32, to = my_band - key0 - c * 32;  // hidden ones of this part
                             if (__all_sync(0xffffffffu, to <= 0 || from >= 32)) continue;
+                            if (__all_sync(0xffffffffu, from <= 0 && to >= 32)) live &= ~(1u << c);
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 if (i >= from && i < to) r[c * 32 + i] = 0xff800000u;  // -inf
@@ -748,15 +751,25 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
                 uint64_t sm2[4] = {0ull, 0ull, 0ull, 0ull};
                 uint32_t pk[kTile / 2];
 #pragma unroll
-                for (int i = 0; i < kTile / 2; ++i) {
-                    const uint64_t t2 = fma_f32x2(pack_f32x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), scale2, shift2);
-                    float e0, e1;
-                    unpack_f32x2(t2, e0, e1);
-                    const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
-                    sm2[i & 3] = add_f32x2(sm2[i & 3], pack_f32x2(p0, p1));
-                    pk[i] = pack_bf16x2(p0, p1);
-                    if (i % 16 == 15) tmem_st16(tP + i - 15, &pk[i - 15]);
-                    if (i == kTurn) pass_on(kPassTurn, wg, quarter);
+                for (int c = 0; c < 4; ++c) {
+                    if ((MODE & 4) && !(live >> c & 1)) {  // nobody of this warp sees a key of this part
+#pragma unroll
+                        for (int i = c * 16; i < c * 16 + 16; ++i) pk[i] = 0u;
+                        if (c == kTurn / 16) pass_on(kPassTurn, wg, quarter);
+                        tmem_st16(tP + c * 16, &pk[c * 16]);
+                        continue;
+                    }
+#pragma unroll
+                    for (int i = c * 16; i < c * 16 + 16; ++i) {
+                        const uint64_t t2 = fma_f32x2(pack_f32x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), scale2, shift2);
+                        float e0, e1;
+                        unpack_f32x2(t2, e0, e1);
+                        const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
+                        sm2[i & 3] = add_f32x2(sm2[i & 3], pack_f32x2(p0, p1));
+                        pk[i] = pack_bf16x2(p0, p1);
+                        if (i % 16 == 15) tmem_st16(tP + i - 15, &pk[i - 15]);
+                        if (i == kTurn) pass_on(kPassTurn, wg, quarter);
+                    }
                 }
                 tmem_wait_st();
                 tc_fence_before_sync();
