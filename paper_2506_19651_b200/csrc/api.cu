@@ -527,10 +527,11 @@ static void add_question(AttnParams& p, const QueryPlan& qp) {
 
 // K and V of one range of each of p.batch sequences: `rows` rows from the base on, the sequences seq_rows apart.  (A map needs at
 // least one row; an empty range is never read.)
-static int kv_maps(AttnMaps& m, int i, const AttnParams& p, int d, const __nv_bfloat16* k, const __nv_bfloat16* v, int64_t rows, int64_t seq_rows) {
+static int kv_maps(AttnMaps& m, int i, const AttnParams& p, int d, const __nv_bfloat16* k, const __nv_bfloat16* v, int64_t rows, int64_t seq_rows,
+                   int k_box = kTile / 2, int v_box = kTile) {
     const int64_t n = rows > 0 ? rows : 1;
-    const int rc = make_tmap(&m.k[i], k, n, p.Hkv, d, 1, kTile / 2, 64, p.batch, seq_rows);
-    return rc != PEVLM_OK ? rc : make_tmap(&m.v[i], v, n, p.Hkv, d, 1, kTile, d / 2, p.batch, seq_rows);
+    const int rc = make_tmap(&m.k[i], k, n, p.Hkv, d, 1, k_box, 64, p.batch, seq_rows);
+    return rc != PEVLM_OK ? rc : make_tmap(&m.v[i], v, n, p.Hkv, d, 1, v_box, d / 2, p.batch, seq_rows);
 }
 
 static int prefill_maps(AttnMaps& m, const AttnParams& p, int d, const __nv_bfloat16* q, const __nv_bfloat16* k, const __nv_bfloat16* v) {
@@ -831,6 +832,7 @@ int pevlm_window_attn(const pevlm_shape_t* s, int32_t window, const void* q, con
     p.first_pos = static_cast<int>(first_token);
     p.window = window < 1 << 30 ? window : 1 << 30;
     p.sink_len = static_cast<int>(s->sink_len < keys ? s->sink_len : keys);
+    p.sink_pad = p.sink_len <= 48 ? (p.sink_len + 15) & ~15 : 0;
     p.block_rows = static_cast<int>(keys);
     p.blk_key0 = 0;
     p.kv_rows = static_cast<int>(cache_rows);
@@ -840,7 +842,12 @@ int pevlm_window_attn(const pevlm_shape_t* s, int32_t window, const void* q, con
         p.keep_status = b > 0;
         const int64_t q0 = b * n_tokens, k0 = b * cache_rows;
         AttnMaps m;
-        if ((rc = prefill_maps(m, p, d, rows_of(q, q0, p.Hq, d), rows_of(k_cache, k0, p.Hkv, d), rows_of(v_cache, k0, p.Hkv, d))) != PEVLM_OK) return rc;
+        const __nv_bfloat16 *k = rows_of(k_cache, k0, p.Hkv, d), *v = rows_of(v_cache, k0, p.Hkv, d);
+        if ((rc = prefill_maps(m, p, d, rows_of(q, q0, p.Hq, d), k, v)) != PEVLM_OK) return rc;
+        if (p.sink_pad > 0) {
+            if ((rc = kv_maps(m, 1, p, d, k, v, p.sink_len, p.kv_rows, p.sink_pad, p.sink_pad)) != PEVLM_OK) return rc;
+            if ((rc = kv_maps(m, 2, p, d, k, v, p.block_rows, p.kv_rows, kTile / 2 - p.sink_pad, kTile - p.sink_pad)) != PEVLM_OK) return rc;
+        }
         p.o = const_cast<__nv_bfloat16*>(rows_of(o, q0, p.Hq, d));
         p.lse = lse ? lse + p.Hq * q0 : nullptr;
         const cudaError_t e = launch_attn(p, d, m, st);

@@ -100,9 +100,10 @@ struct QSlot {
 // The own range is fetched at row b_coord0 of the block tensor map (own_map = 0), for the sink's own items of the sink map
 // (1), for question items of the map of the whole cache (2).  seq: sequence of the batch, a dimension of those maps of its own.
 // n_a, n_b: MMA columns of tile na - 1 and of the last tile; the others have 128.
-// Sliding window: keys of the own range from band on are hidden up to a row's band_end0 + token of the row.
+// Sliding window: keys of the own range from band on are hidden up to a row's band_end0 + token of the row (at least up to pad).  pad > 0:
+// the own range begins with the sink, padded to that many keys, in the first tile; its own keys follow (see decode_item).
 struct WorkItem {
-    int band;
+    int band, pad;
     int kv_head, a_end, na, nt, n_a, n_b, split, b_coord0, own_map, seq;
     QSlot s[2];
 };
@@ -180,13 +181,15 @@ __device__ __forceinline__ void decode_item(const AttnParams& p, int w, WorkItem
         }
         if ((MODE & 4) && own_keys > 0) {
             // The own range starts where the window of the pair's first row does, or at key 0 where that is within or right behind
-            // the sink: then it takes the sink in, whose keys the window does not hide.
+            // the sink: then it takes the sink in, whose keys the window does not hide.  A short sink does not get a key tile of its own
+            // (a tile takes its time whatever there is in it): it stands in front of the own keys, in their first tile.
             const int low = it.s[1].valid ? min(it.s[0].limit0, it.s[1].limit0) : it.s[0].limit0;
             const int start = p.first_pos + low - p.window + 1;
             const bool apart = start > p.sink_len;
-            it.a_end = apart ? p.sink_len : 0;
-            it.b_coord0 = apart ? start : 0;
-            it.band = apart ? 0 : p.sink_len;
+            it.pad = apart ? p.sink_pad : 0;
+            it.a_end = apart && it.pad == 0 ? p.sink_len : 0;
+            it.b_coord0 = apart ? start - it.pad : 0;
+            it.band = apart && it.pad == 0 ? 0 : p.sink_len;
             own_keys += p.first_pos - it.b_coord0;
 #pragma unroll 1
             for (int x = 0; x < 2; ++x) {
@@ -234,6 +237,7 @@ __device__ __forceinline__ void decode_item(const AttnParams& p, int w, WorkItem
     it.nt = own_keys > 0 ? it.na + cdiv(own_keys, kTile) : 0;
     it.n_a = (it.a_end - (it.na - 1) * kTile + 15) & ~15;
     it.n_b = (own_keys - (it.nt - it.na - 1) * kTile + 15) & ~15;
+    if ((MODE & 4) && it.nt == 1 && it.pad > 0) it.n_b = kTile;  // its halves are those of a whole tile
 }
 
 // Between the two softmax warps that share a scheduler (warp `quarter` of each warpgroup), hardware barriers of 64
@@ -430,7 +434,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
             {
                 // The K cursor's item, and where V has to come from: the rows of the last kQkAhead K tiles (base row of the
                 // tile, kv head and map, sequence), the V tile of a step being that of kQkAhead steps ago.
-                int k = -1, j = 0, nt = 0, na = 0, n_a = 0, n_b = 0, kv_head = 0, b_coord0 = 0, own_map = 0, seq = 0;
+                int k = -1, j = 0, nt = 0, na = 0, n_a = 0, n_b = 0, kv_head = 0, b_coord0 = 0, own_map = 0, seq = 0, pad = 0;
                 int v_row[kQkAhead], v_from[kQkAhead], v_seq[kQkAhead];
                 uint32_t tiles = 0;  // K tiles loaded so far
                 bool more = true;
@@ -445,6 +449,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
                             nt = uniform(it.nt); na = uniform(it.na); n_a = uniform(it.n_a); n_b = uniform(it.n_b);
                             kv_head = uniform(it.kv_head); b_coord0 = uniform(it.b_coord0); own_map = uniform(it.own_map);
                             seq = uniform(it.seq);
+                            if (MODE & 4) pad = uniform(it.pad);
                             const int qm = uniform(q.qmap), q_head0 = uniform(q.q_head0), q_tok0 = uniform(q.q_tok0);
                             const int valid = uniform(q.valid);
                             const int rows = uniform((it.s[0].valid ? it.s[0].box_rows : 0) + (it.s[1].valid ? it.s[1].box_rows : 0));
@@ -477,10 +482,21 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
                         if (tiles >= kRing) wait_s_full(tiles - kRing, kWaitKvFree);
                         if (rank == 0 && lane == 0) mbar_arrive_expect_tx(smem_u32(&bars.k_full[slot]), 2 * L::kKBytes);
                         const uint32_t bar = map_to_cta(smem_u32(&bars.k_full[slot]), 0);
+                        if ((MODE & 4) && pad > 0 && j == 0) from = kv_head * 4 + 3;
+                        if ((MODE & 4) && pad > 0 && j == 0 && rank == 0) {
+                            // map 1: the sink, a box of pad keys; map 2: the own keys, a box of the rest
 #pragma unroll 1
-                        for (int h = 0; h < NP; ++h)
-                            tma_load_4d_pair(smem_base + L::kK + slot * L::kKBytes + h * L::kKPanelBytes, &maps.k[map], h * 64, kv_head,
-                                             row + static_cast<int>(rank) * (n >> 1), seq, bar);
+                            for (int h = 0; h < NP; ++h) {
+                                const uint32_t to = smem_base + L::kK + slot * L::kKBytes + h * L::kKPanelBytes;
+                                tma_load_4d_pair(to, &maps.k[1], h * 64, kv_head, 0, seq, bar);
+                                tma_load_4d_pair(to + pad * 128, &maps.k[2], h * 64, kv_head, row + pad, seq, bar);
+                            }
+                        } else {
+#pragma unroll 1
+                            for (int h = 0; h < NP; ++h)
+                                tma_load_4d_pair(smem_base + L::kK + slot * L::kKBytes + h * L::kKPanelBytes, &maps.k[map], h * 64, kv_head,
+                                                 row + static_cast<int>(rank) * (n >> 1), seq, bar);
+                        }
                         ++j;
                         ++tiles;
                     }
@@ -488,8 +504,13 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
                         const uint32_t u = s - kQkAhead, slot = u % kRing;
                         if (u >= kRing) wait_pv_done(u - kRing, kWaitKvFree);
                         if (rank == 0 && lane == 0) mbar_arrive_expect_tx(smem_u32(&bars.v_full[slot]), 2 * L::kVBytes);
-                        tma_load_4d_pair(smem_base + L::kV + slot * L::kVBytes, &maps.v[v_from[0] & 3], static_cast<int>(rank) * (D / 2),
-                                         v_from[0] >> 2, v_row[0], v_seq[0], map_to_cta(smem_u32(&bars.v_full[slot]), 0));
+                        const uint32_t to = smem_base + L::kV + slot * L::kVBytes, bar = map_to_cta(smem_u32(&bars.v_full[slot]), 0);
+                        if ((MODE & 4) && (v_from[0] & 3) == 3) {
+                            tma_load_4d_pair(to, &maps.v[1], static_cast<int>(rank) * (D / 2), v_from[0] >> 2, 0, v_seq[0], bar);
+                            tma_load_4d_pair(to + p.sink_pad * D, &maps.v[2], static_cast<int>(rank) * (D / 2), v_from[0] >> 2, v_row[0] + p.sink_pad, v_seq[0], bar);
+                        } else {
+                            tma_load_4d_pair(to, &maps.v[v_from[0] & 3], static_cast<int>(rank) * (D / 2), v_from[0] >> 2, v_row[0], v_seq[0], bar);
+                        }
                     }
 #pragma unroll
                     for (int i = 0; i < kQkAhead - 1; ++i) {
@@ -658,7 +679,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ AttnMa
             const int end = uniform(qs.valid ? qs.end : 0), first_limit = uniform(qs.limit0);
             const int my_limit = min(first_limit + row_tok, end - 1), limit0 = min(first_limit, end - 1);
             // sliding window: the row's hidden keys [band, my_band), and the most that a row of the tile has
-            const int band = uniform(it.band), my_band = qs.band_end0 + row_tok, last_band = uniform(qs.band_end0) + uniform(qs.ntok) - 1;
+            const int band = uniform(it.band), my_band = max(it.pad, qs.band_end0 + row_tok);
+            const int last_band = uniform(max(it.pad, qs.band_end0 + qs.ntok - 1));
             __syncwarp();
             if (lane == 0) item_release(k);
             if (k == 0) grid_wait();

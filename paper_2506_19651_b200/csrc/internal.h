@@ -138,6 +138,7 @@ struct AttnParams {
     int32_t keep_status;    // a later launch of the same call
     int32_t first_pos;      // sliding window: position of the first row,
     int32_t window;         // and positions that a row sees, its own among them (beside the first sink_len)
+    int32_t sink_pad;       // a sink of at most 48 keys shares the first tile of a window, padded to a multiple of 16 (0: it does not)
 };
 
 constexpr int kMergeRows = 8 * kNumSms;  // most rows of the merge that takes a CTA for each (as many as are resident)
@@ -269,7 +270,8 @@ cudaError_t launch_copy_segments(const CopySegments& s, cudaStream_t stream);
 //   q[0]: [rows, Hq, d] with a 128-token box; q[1 + kind]: the same tensor with the box of the segment kind's packed ragged
 //   tail (heads x tail rows); q[4]: the question rows (box: one kv group's heads x the tokens of a tile)
 //   k, v[0]: the context blocks of the call (base at the first block's row); [1]: the sink, rows [0, S), so that a ragged
-//   last key tile of either range reads zeros past its end instead of a neighbour's rows; [2]: the whole cache.  The
+//   last key tile of either range reads zeros past its end instead of a neighbour's rows; [2]: the whole cache.  (Sliding window: [0] the
+//   whole cache; where the sink shares a tile, [1] has a box of sink_pad keys and [2] is the cache with a box of the rest.)  The
 //   sequences of a batch are the maps' last dimension, so that the end of the range is the end of the map in each of them
 struct AttnMaps {
     CUtensorMap q[5], k[3], v[3];

@@ -82,6 +82,9 @@ PREFILL = [
     (640, 0, 129, 127, 3, 1, 64), (900, 0, 300, 64, 28, 4, 128), (257, 0, 5000, 3, 4, 2, 64), (600, 0, 200, 1000, 4, 2, 64), (640, 0, 33, 300, 7, 1, 128),
     (200, 1, 150, 16, 14, 2, 128), (150, 700, 128, 8, 7, 1, 128), (129, 333, 77, 130, 5, 1, 64), (48, 1000, 256, 4, 28, 4, 128), (97, 2000, 2 ** 31 - 1, 2, 4, 2, 64),
     (33, 90, 60, 40, 8, 8, 64), (385, 0, 256, 0, 8, 1, 64), (100, 5, 3, 1, 32, 8, 128), (2100, 0, 777, 4, 2, 1, 128),
+    # sinks that share the window's first tile and sinks just too long for it, windows of one tile
+    (700, 0, 100, 17, 4, 2, 64), (700, 0, 100, 48, 7, 1, 128), (700, 0, 100, 49, 4, 2, 128), (500, 900, 90, 33, 3, 1, 64), (500, 900, 300, 47, 4, 2, 128),
+    (40, 500, 10, 5, 8, 8, 64), (40, 500, 10, 48, 8, 8, 128), (40, 500, 1, 16, 8, 8, 128), (129, 500, 2, 1, 4, 4, 64), (300, 40, 9, 31, 5, 1, 128),
 ]
 FEW = [
     (1, 0, 1, 0, 4, 2, 64), (1, 0, 10, 5, 7, 1, 128), (1, 15, 16, 0, 4, 2, 64), (1, 16, 16, 0, 4, 2, 64), (1, 5000, 100, 4, 28, 4, 128), (1, 5000, 4096, 64, 32, 8, 64),
