@@ -583,7 +583,7 @@ __global__ void __launch_bounds__(RPB * TURNS * 32) packed_merge_kernel(const __
     float top = kNoMax, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (some) {
-        constexpr int kAtOnce = 5;  // of a warp's shares, in flight together, with the first maxima
+        constexpr int kAtOnce = RPB * TURNS <= 16 ? 10 : 5;  // of a warp's shares, in flight together, with the first maxima
         float4 v[kAtOnce];
         float m[kAtOnce], l[kAtOnce];
         auto load = [&](int first) {
