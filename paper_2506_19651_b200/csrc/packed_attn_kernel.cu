@@ -186,22 +186,29 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
         uint32_t q[NT][KS][2];
         float sc[NT][2];
         int pos[NT][2];
-        auto rows_of_unit = [&]() {
+        uint32_t raw_q[NT][KS * 2];
+        auto ask_for_rows = [&]() {
             const int rows = min(cur.s.n * p.G - cur.chunk * L::kRows, L::kRows);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 const int rr = cur.chunk * L::kRows + 8 * j + g;
-                uint32_t x[KS * 2];
-                float top = 0.f;
                 if (8 * j + g < rows) {
                     const int tok = quotient(rr, p.div_g), h = cur.head * p.G + rr - tok * p.G;
                     const __nv_bfloat16* src = p.q + (cur.s.row0 + tok) * p.q_stride + h * D + t * (D / 4);
 #pragma unroll
-                    for (int c = 0; c < KS / 2; ++c) *reinterpret_cast<uint4*>(&x[4 * c]) = reinterpret_cast<const uint4*>(src)[c];  // through L1: all warps of the SM read these rows
+                    for (int c = 0; c < KS / 2; ++c) *reinterpret_cast<uint4*>(&raw_q[j][4 * c]) = reinterpret_cast<const uint4*>(src)[c];  // through L1: all warps of the SM read these rows
                 } else {
 #pragma unroll
-                    for (int c = 0; c < KS * 2; ++c) x[c] = 0u;
+                    for (int c = 0; c < KS * 2; ++c) raw_q[j][c] = 0u;
                 }
+            }
+        };
+        auto rows_of_unit = [&]() {
+            const int rows = min(cur.s.n * p.G - cur.chunk * L::kRows, L::kRows);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                uint32_t (&x)[KS * 2] = raw_q[j];
+                float top = 0.f;
 #pragma unroll
                 for (int c = 0; c < KS * 2; ++c) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(x[c] << 16)), fabsf(__uint_as_float(x[c] & 0xffff0000u))));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -231,7 +238,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                 asm volatile("prefetch.global.L1 [%0];" ::"l"(p.q + (u.s.row0 + tok) * p.q_stride + h * D + x % kLines * 64));
             }
         };
-        rows_of_unit();  // the first ones while the first places are looked up
+        ask_for_rows();
         uint32_t places = place_of(ahead, block + lane, page);
         unsigned there = 0;  // two bits a step, the latest in the lowest: the tiles exist
         const uint8_t* const cache = p.cache + lane * 16;
@@ -279,6 +286,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         for (int i = 0; i < L::kStages - 1; ++i) fetch();
+        rows_of_unit();
 
         uint32_t from_place = 0;
         bool first_unit = true;
@@ -287,7 +295,10 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
             const int tiles = tiles_of(cur, unit0) - first_tile;
             const int rows = min(cur.s.n * p.G - cur.chunk * L::kRows, L::kRows);
             float m[NT][2], l[NT][2], o[NT][MT][4];
-            if (!first_unit) rows_of_unit();
+            if (!first_unit) {
+                ask_for_rows();
+                rows_of_unit();
+            }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
 #pragma unroll
@@ -631,7 +642,9 @@ static cudaError_t launch_rows(const PackedAttnParams& p, cudaStream_t stream) {
     using L = PackedAttnLayout<D, NT>;
     const cudaError_t e = launch_chained<packed_attn_kernel<D, NT>>(dim3(kNumSms), L::kWarps * 32, L::kTotal, stream, p);
     if (e != cudaSuccess) return e;
-    return launch_chained<packed_merge_kernel<D, 8 * NT, 4 * NT, 4>>(dim3(kNumSms - 1, 2), 16 * NT * 32, 0, stream, p);
+    // (measured: 8 rows in halves with four turns 17.5 us for one token against 50K keys, as a whole with two 18.9; 16 rows as a whole with one
+    // turn 27.4 us for 16 sequences under a window, in halves with four 30.7)
+    return launch_chained<packed_merge_kernel<D, 8 * NT, NT == 1 ? 4 : 16, NT == 1 ? 4 : 1>>(dim3(kNumSms - 1, NT == 1 ? 2 : 1), 512, 0, stream, p);
 }
 
 template <int D>
