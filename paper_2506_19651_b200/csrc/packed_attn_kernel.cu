@@ -48,10 +48,16 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
         const int each = (p.num_seqs + 31) / 32, r0 = lane * each;
         PackedSeq s[kSeqsPerLane];
         int64_t upto[kSeqsPerLane], mine = 0;
+        int len[kSeqsPerLane], start[kSeqsPerLane + 1];  // all in flight together
+#pragma unroll
+        for (int i = 0; i <= kSeqsPerLane; ++i) {
+            if (i < kSeqsPerLane) len[i] = i < each && r0 + i < p.num_seqs ? p.lens[r0 + i] : 0;
+            start[i] = i <= each && r0 + i <= p.num_seqs ? p.row_start[r0 + i] : 0;
+        }
 #pragma unroll
         for (int i = 0; i < kSeqsPerLane; ++i) {
             s[i] = {0, 0, 0, 0, 1, 0, 0};
-            if (i < each && r0 + i < p.num_seqs) table[r0 + i] = s[i] = packed_seq<4>(p, r0 + i, rows_per_chunk);
+            if (i < each && r0 + i < p.num_seqs) table[r0 + i] = s[i] = packed_seq<4>(p, len[i], start[i], start[i + 1], rows_per_chunk);
             mine += seq_tiles<4>(p, s[i]);
             upto[i] = mine;
         }
@@ -577,7 +583,8 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
 // Units that cross from one worker (a CTA of packed_attn_kernel, a pair of packed_tile_kernel) into the next: blocks (c, y) take the one
 // that worker c - the first of it - ends with, RPB of its rows each.  A warp for every row and every TURNS-th of the workers, lanes are
 // columns; the warps of a row meet in shared memory.
-template <int D, int ROWS, int RPB, int TURNS>
+// AT_ONCE: of a warp's shares, in flight together, with the first maxima.
+template <int D, int ROWS, int RPB, int TURNS, int AT_ONCE>
 __global__ void __launch_bounds__(RPB * TURNS * 32) packed_merge_kernel(const __grid_constant__ PackedAttnParams p) {
     constexpr int kTurns = TURNS, kShareFloats = ROWS * (D + 2);
     __shared__ float4 s_acc[kTurns][RPB][32];
@@ -594,12 +601,11 @@ __global__ void __launch_bounds__(RPB * TURNS * 32) packed_merge_kernel(const __
     float top = kNoMax, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (some) {
-        constexpr int kAtOnce = RPB * TURNS <= 16 ? 10 : 5;  // of a warp's shares, in flight together, with the first maxima
-        float4 v[kAtOnce];
-        float m[kAtOnce], l[kAtOnce];
+        float4 v[AT_ONCE];
+        float m[AT_ONCE], l[AT_ONCE];
         auto load = [&](int first) {
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
+            for (int i = 0; i < AT_ONCE; ++i) {
                 const int c = min(first + i * kTurns, c1);
                 const float* const share = share_of(c);
                 m[i] = __ldcg(share + ROWS * D + row);
@@ -611,10 +617,10 @@ __global__ void __launch_bounds__(RPB * TURNS * 32) packed_merge_kernel(const __
         for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(share_of(c) + ROWS * D + row));
 #pragma unroll
         for (int by = 16; by > 0; by /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, by));
-        for (int c = c0 + turn; c <= c1; c += kAtOnce * kTurns) {
+        for (int c = c0 + turn; c <= c1; c += AT_ONCE * kTurns) {
             if (c > c0 + turn) load(c);
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
+            for (int i = 0; i < AT_ONCE; ++i) {
                 const float f = c + i * kTurns <= c1 ? fast_exp2(m[i] - top) : 0.f;
                 sum += f * l[i];
                 acc.x += f * v[i].x; acc.y += f * v[i].y; acc.z += f * v[i].z; acc.w += f * v[i].w;
@@ -642,16 +648,20 @@ static cudaError_t launch_rows(const PackedAttnParams& p, cudaStream_t stream) {
     using L = PackedAttnLayout<D, NT>;
     const cudaError_t e = launch_chained<packed_attn_kernel<D, NT>>(dim3(kNumSms), L::kWarps * 32, L::kTotal, stream, p);
     if (e != cudaSuccess) return e;
-    // (measured: 8 rows in halves with four turns 17.5 us for one token against 50K keys, as a whole with two 18.9; 16 rows as a whole with one
-    // turn 27.4 us for 16 sequences under a window, in halves with four 30.7)
-    return launch_chained<packed_merge_kernel<D, 8 * NT, NT == 1 ? 4 : 16, NT == 1 ? 4 : 1>>(dim3(kNumSms - 1, NT == 1 ? 2 : 1), 512, 0, stream, p);
+    // Few units have many shares each (a unit alone those of all CTAs): ten of a row in flight, whose registers leave a CTA to an SM, i.e. two rounds
+    // of them.  Many units have two or three: five, and one round.  Measured, ten against five: one token against 50K keys 17.5 / 18.1 us, 64 sequences
+    // of up to 16K 75.0 / 72.5.  (8 rows as a whole with two turns 18.9 and 16 rows in halves with four 30.7 us for 16 sequences under a
+    // window, as a whole with one turn 27.4.)
+    if (NT == 2) return launch_chained<packed_merge_kernel<D, 16, 16, 1, 10>>(dim3(kNumSms - 1), 512, 0, stream, p);
+    if (static_cast<int64_t>(p.num_seqs) * p.Hkv <= 32) return launch_chained<packed_merge_kernel<D, 8, 4, 4, 10>>(dim3(kNumSms - 1, 2), 512, 0, stream, p);
+    return launch_chained<packed_merge_kernel<D, 8, 4, 4, 5>>(dim3(kNumSms - 1, 2), 512, 0, stream, p);
 }
 
 template <int D>
 static cudaError_t launch_tiles(const PackedAttnParams& p, cudaStream_t stream) {
     const cudaError_t e = launch_packed_tile(p, D, stream);
     if (e != cudaSuccess) return e;
-    return launch_chained<packed_merge_kernel<D, 2 * kTile, 8, 1>>(dim3(kNumSms / 2 - 1, 2 * kTile / 8), 8 * 32, 0, stream, p);
+    return launch_chained<packed_merge_kernel<D, 2 * kTile, 8, 1, 5>>(dim3(kNumSms / 2 - 1, 2 * kTile / 8), 8 * 32, 0, stream, p);
 }
 
 // Measured, few rows against tiles: 28/4 heads of 128, 50K keys 28 rows 29.7 / 34.6 us, 35 rows 36.6 / 34.7, 56 rows 43.6 / 35.9; 64 sequences of

@@ -22,12 +22,13 @@ struct PackedSeq {
     int ns, skip;          // tiles from ns on are skip tiles further on in the sequence (between sink and window nobody looks)
 };
 
+// From what the sequence's lens[r], row_start[r] and row_start[r + 1] hold.
 template <int TS>
-__device__ __forceinline__ PackedSeq packed_seq(const PackedAttnParams& p, int r, int rows_per_chunk) {
+__device__ __forceinline__ PackedSeq packed_seq(const PackedAttnParams& p, int len, int from, int to, int rows_per_chunk) {
     PackedSeq s;
-    s.len = min(max(p.lens[r], 0), p.max_pages << p.page_shift);
-    s.row0 = min(max(p.row_start[r], 0), p.n_rows);
-    s.n = max(min(p.row_start[r + 1], p.n_rows) - s.row0, 0);
+    s.len = min(max(len, 0), p.max_pages << p.page_shift);
+    s.row0 = min(max(from, 0), p.n_rows);
+    s.n = max(min(to, p.n_rows) - s.row0, 0);
     s.chunks = (s.n * p.G + rows_per_chunk - 1) / rows_per_chunk;
     s.ns = s.skip = 0;
     constexpr int kKeys = 1 << TS;
@@ -39,6 +40,11 @@ __device__ __forceinline__ PackedSeq packed_seq(const PackedAttnParams& p, int r
     }
     s.cnt = max(tiles - s.skip, 1);  // a sequence without keys has a tile that nothing is visible in
     return s;
+}
+
+template <int TS>
+__device__ __forceinline__ PackedSeq packed_seq(const PackedAttnParams& p, int r, int rows_per_chunk) {
+    return packed_seq<TS>(p, p.lens[r], p.row_start[r], p.row_start[r + 1], rows_per_chunk);
 }
 
 // a / b for a >= 0, b > 0: 32 bits wherever they do (a 64-bit division is a subroutine of a hundred instructions).
