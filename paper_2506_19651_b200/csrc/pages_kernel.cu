@@ -106,22 +106,23 @@ __global__ void __launch_bounds__(THREADS) assign_kernel(const __grid_constant__
             s_len[tid] = granted ? len : -1 - len;
             s_top[tid] = static_cast<int>(count - 1 - (to.pages - need) + have);
             __syncthreads();
-            const int64_t lo = max(first, row0), hi = min(last, row1);
-            for (int64_t g = lo / ROWS * ROWS + ROWS * tid; g < hi; g += ROWS * THREADS) {
-                int q = last_at_or_before(s_start, n, static_cast<int>(max(g, lo)));
+            // (rows and positions fit 31 bits: at most 2^30 rows, and a position is below the 2^30 of a table's row or that many behind it)
+            const int lo = static_cast<int>(max(first, row0)), hi = static_cast<int>(min(last, row1));
+            for (int g = lo / ROWS * ROWS + ROWS * tid; g < hi; g += ROWS * THREADS) {
+                int q = last_at_or_before(s_start, n, max(g, lo));
                 int slot[ROWS], position[ROWS], page = -1, page_q = -1, page_index = -1;  // neighbours mostly share a page
 #pragma unroll
                 for (int i = 0; i < ROWS; ++i) {
-                    const int64_t row = g + i;
+                    const int row = g + i;
                     slot[i] = -1;
                     position[i] = 0;
                     if (row < lo || row >= hi) continue;
                     while (q + 1 < n && s_start[q + 1] <= row) ++q;  // sequences without rows are passed over
                     const int held = s_len[q] < 0 ? -1 - s_len[q] : s_len[q];
-                    const int64_t pos = held + (row - s_start[q]);
-                    position[i] = static_cast<int>(min(pos, static_cast<int64_t>(INT32_MAX)));
+                    const int pos = held + (row - s_start[q]);
+                    position[i] = pos;
                     if (s_len[q] < 0) continue;
-                    const int index = static_cast<int>(pos >> p.page_shift);
+                    const int index = pos >> p.page_shift;
                     if (q != page_q || index != page_index) {
                         int32_t* const entry = p.page_table + static_cast<int64_t>(r0 + q) * p.max_pages + index;
                         const bool fresh = index >= (held + P - 1) >> p.page_shift;
@@ -130,11 +131,14 @@ __global__ void __launch_bounds__(THREADS) assign_kernel(const __grid_constant__
                         page_index = index;
                         if (fresh && (pos & (P - 1)) == 0) *entry = page;
                     }
-                    if (page >= 0 && page < p.num_pages) slot[i] = (page << p.page_shift) + static_cast<int>(pos & (P - 1));
+                    if (page >= 0 && page < p.num_pages) slot[i] = (page << p.page_shift) + (pos & (P - 1));
                 }
-                if (ROWS == 4 && g >= lo && g + 4 <= hi) {
-                    *reinterpret_cast<int4*>(p.slots + g) = make_int4(slot[0], slot[1 % ROWS], slot[2 % ROWS], slot[3 % ROWS]);
-                    *reinterpret_cast<int4*>(p.positions + g) = make_int4(position[0], position[1 % ROWS], position[2 % ROWS], position[3 % ROWS]);
+                if (ROWS % 4 == 0 && g >= lo && g + ROWS <= hi) {
+#pragma unroll
+                    for (int i = 0; i + 3 < ROWS; i += 4) {
+                        *reinterpret_cast<int4*>(p.slots + g + i) = make_int4(slot[i], slot[i + 1], slot[i + 2], slot[i + 3]);
+                        *reinterpret_cast<int4*>(p.positions + g + i) = make_int4(position[i], position[i + 1], position[i + 2], position[i + 3]);
+                    }
                 } else {
 #pragma unroll
                     for (int i = 0; i < ROWS; ++i) {
