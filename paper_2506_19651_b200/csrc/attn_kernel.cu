@@ -36,6 +36,9 @@
 //     instantiation per mode, loops that stay loops wherever the registers' indices allow it, waits that expand to
 //     little, no divisions, and warp-uniform values that the compiler knows to be uniform (the MMA warps' descriptors
 //     then live in uniform registers instead of being moved there for every MMA: 10 KB of code).
+// A sliding window (MODE bit 2) is a kind of work item: the key tiles of the first tokens and those from the window of the pair's first row to the
+// diagonal, with a band of hidden keys in front.  A 128-row tile needs window + 127 keys, so short windows pay for masked columns: 12.6K tokens
+// under 777 positions beside 4 (28/4 heads) 181 us = 752 TFLOP/s of visible pairs, 50K under 2,048 beside 64 1,442 us = 1,030, both at the power cap.
 // Every wait on an mbarrier is bounded; an expired wait records PEVLM_ETIMEOUT and the CTA still runs to its
 // normal end (waits become short) and stays until what is in flight has landed, so TMEM is always released and nothing
 // writes to shared memory that has a new owner.

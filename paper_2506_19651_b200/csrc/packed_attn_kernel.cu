@@ -19,8 +19,13 @@
 // free), the rows of V^T are elements 16 g + 2 i, + 1, so a thread needs 16 bytes of codes of two keys, 8 bytes of four, and one scale for
 // all of them.  Probabilities change from the result's layout to the operand's by movmatrix.
 // Rows of Q are scaled by a power of two to at most 2 in magnitude, so that any bf16 values fit fp16 (what is below 2^-24 of the
-// row's largest is lost, far below fp32's rounding of the sum); sums, maxima and outputs are fp32.  Probabilities are rounded to fp16
-// (2^-11 of each; 2^-24 of the row's largest where smaller).
+// row's largest is lost, as it would be in fp32's rounding of the sum); sums, maxima and outputs are fp32.  Probabilities are rounded to fp16
+// (2^-11 of each; 2^-25 of the running reference where smaller).
+// What bounds it: large batches HBM (64 sequences of up to 16K keys, 28/4 heads: 304 MB at 6 TB/s while the warps are in their loops, 55 of 72 us;
+// the start, the slowest warps, the join and the merge are the rest); small ones the chain lengths -> part -> pages -> tiles -> join -> merge
+// and the instructions (277 of a warp a tile of 16 keys, 128 of them the conversions and the products with the scales; half of the ALU's
+// throughput, which conversions share, is in use).  One token against 50K keys (29 MB) 17.5 us, of which 6 in the loop; 16 sequences of heads of
+// 64 under a window (38 MB) 27.8.  Two tiles a step (two chains of dependent products): 116 -> 77.5 us for the 64 sequences.
 #include "packed_list.cuh"
 
 namespace pevlm {

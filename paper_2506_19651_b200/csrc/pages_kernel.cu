@@ -5,7 +5,8 @@
 // chain  lengths -> sums -> which sequence a row belongs to -> page -> slot.  So one launch does all of it: every CTA forms the sums
 // of all sequences itself (1,024 at a time, a thread each), instead of waiting for one that does, and then serves its own part of the rows, finding
 // a row's sequence by bisection in shared memory.  That needs inputs that nobody writes meanwhile, hence the rule that outputs are
-// not inputs.
+// not inputs.  Both calls of a step of 64 sequences take 4.8 us on the GPU (the host, which needs 3.5 us a call, is the bound there), 700 arrivals with
+// room for 1.1M rows 11 us, 8.9 MB of it written in about 4.
 #include "internal.h"
 #include "ptx.cuh"
 
