@@ -220,7 +220,7 @@ int pevlm_layer_forward(const pevlm_shape_t* shape, int32_t last_len, const void
  * counts) or j < sink_len (of shape).  One call serves a whole prefill (first_token = 0), a chunk of one behind a cache, and single
  * tokens (few rows take a kernel of their own, like those of pevlm_query_attn).
  *   q [n_tokens, Hq, d] roped; k_cache, v_cache [cache_rows, Hkv, d], of which rows [0, first_token + n_tokens) may be read
- *   (cache_rows >= that); o [n_tokens, Hq, d] (32-byte aligned), lse [Hq, n_tokens] (may be NULL)
+ *   (cache_rows >= that; rows that no row of the call sees are not read: they may hold anything); o [n_tokens, Hq, d] (32-byte aligned), lse [Hq, n_tokens] (may be NULL)
  * batch > 1: sequences of equal lengths, n_tokens rows of q and o, cache_rows rows of the caches apart.  Of `shape` batch, sink_len, the head
  * counts, head_dim and softmax_scale are used.  window >= 1; first_token + n_tokens <= 2^30.
  * workspace: >= pevlm_window_workspace_bytes(...) bytes, 256-byte aligned; that of a call does for any first_token and window.
@@ -317,7 +317,7 @@ int pevlm_packed_load(const pevlm_shape_t* shape, const pevlm_pages_t* pages, co
  *   pevlm_pages_assign leaves them;  o [n_rows, Hq, d] bf16, lse [Hq, n_rows] fp32 (may be NULL), written
  *   max_rows: most rows of one sequence, as the caller knows it (n_rows if not): chooses the kernel, a larger row count stays correct
  * A row that sees no key (a length of 0, or fewer keys than rows) has output 0 and LSE -inf.  Keys in a page whose table entry is outside
- * [0, num_pages) count as not there.  Rows of q that no sequence has are not read, and of o and lse not written.  Scores of finite rows are formed from fp16
+ * [0, num_pages) count as not there, and what keys hold that no row sees (behind the length, in front of the windows) does not matter.  Rows of q that no sequence has are not read, and of o and lse not written.  Scores of finite rows are formed from fp16
  * operands (the cache's values are exact in it) and summed in fp32, probabilities rounded to fp16.
  * workspace: >= pevlm_packed_workspace_bytes(...) bytes, 256-byte aligned, needs no value; two calls at a time need two.
  */

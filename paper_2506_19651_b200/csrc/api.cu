@@ -762,6 +762,7 @@ static QueryPlan plan_window(const pevlm_shape_t* s, int32_t window, int64_t fir
         p->window = window < 1 << 30 ? window : 1 << 30;
         p->sink = static_cast<int32_t>(sink);
         p->sink_pieces = sink_pieces;
+        p->low = low > 0 ? static_cast<int32_t>(low) : 0;
         p->skip = skip;
     }
     return q;

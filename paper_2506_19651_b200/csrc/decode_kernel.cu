@@ -95,8 +95,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) decode_kernel(const __grid_
                 const int row = (i * 32 + lane) / CH, c = lane % CH;
                 const int64_t key = key0 + row;
                 const uint32_t dst = stage + row * ROW + ((c ^ (row & 7)) << 4);
-                const int n_bytes = key < p.L ? 16 : 0;  // past the end: zeros
-                const int64_t off = (key < p.L ? key : 0) * row_stride + c * 8;
+                const bool some = key < p.L && (!WINDOW || key < p.sink || key >= p.low);  // others: zeros
+                const int n_bytes = some ? 16 : 0;
+                const int64_t off = (some ? key : 0) * row_stride + c * 8;
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(k + off), "r"(n_bytes) : "memory");
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + kPiece * ROW), "l"(v + off), "r"(n_bytes) : "memory");
             }

@@ -161,6 +161,7 @@ struct DecodeParams {
     // sliding window (0: none) beside the first `sink` keys; pieces from sink_pieces on are `skip` further on, where nothing between
     // the sink and the window of the first row is visible
     int32_t window, sink, sink_pieces, skip;
+    int32_t low;  // first key of the first row's window: of those before it only the sink is read
 };
 
 struct MergeParams {

@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                     vs[x][0] = scale_pair(vb);
                     vs[x][1] = scale_pair(vb >> 16);
                 }
-                // masks, and scales of 0 for what is behind the end or not there (its bytes may be anything)
+                // masks, and scales of 0 for V of keys that no row sees, whose bytes may be anything
                 if (exist != 3u || n < open_from || n + 1 >= open_to) {
                     const int key0[2] = {cur.key0(n), cur.key0(n + 1)};
 #pragma unroll
@@ -392,8 +392,10 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                             }
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            if (!is_there || key0[x] + 8 * h + 2 * t >= cur.s.len) vs[x][h] = 0u;
-                            else if (key0[x] + 8 * h + 2 * t + 1 >= cur.s.len) vs[x][h] &= 0xffffu;
+                            const int key = key0[x] + 8 * h + 2 * t;
+                            auto nobody_sees = [&](int k) { return !is_there || k >= cur.s.len || (p.window > 0 && k <= pos_min - p.window && k >= p.sink); };
+                            if (nobody_sees(key)) vs[x][h] &= 0xffff0000u;
+                            if (nobody_sees(key + 1)) vs[x][h] &= 0x0000ffffu;
                         }
                     }
                 }

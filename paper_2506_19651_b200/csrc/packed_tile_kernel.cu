@@ -155,6 +155,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
     __shared__ float2 s_sums[kTileSums][2][kTile];
     __shared__ float s_scale[4][kTile];       // softmax scale of the rows in units of log2, items in turn
     __shared__ unsigned s_raw_there[kRawRing], s_there[kFedRing];  // of a tile's 16-key parts, which exist
+    __shared__ __align__(4) uint16_t s_raw_seen[kRawRing][8];  // of each part's keys, those that a row of the item can see
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = same_in_warp(tid >> 5);
@@ -285,6 +286,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
             for (int k = 0; same_in_warp(item_ready(k)); ++k) {
                 const TileItem& it = s_items[k % kTileItems];
                 const int nt = it.nt, t0 = it.t0, ns = it.ns, skip = it.skip, len = it.len, head = it.head, seq = it.seq;
+                const int low = p.window > 0 ? len - it.n + quotient(it.chunk * L::kRows, p.div_g) - p.window + 1 : 0;  // of the first row's window
                 __syncwarp();
                 if (lane == 0) item_release(k);
                 auto sub = [&](int j) { return (j < ns ? j : j + skip) * 8 + lane; };  // of the sequence's 16-key tiles
@@ -297,6 +299,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                     const uint32_t at = lane < 8 ? packed_place(p, page, head, sub(j), L::kSubBytes / 128) : kNoTile;
                     const unsigned there = __ballot_sync(0xffffffffu, at != kNoTile);
                     const uint32_t bar = smem_u32(&bars.raw_full[place]);
+                    if (lane < 8) {
+                        const int key0 = sub(j) << 4;
+                        auto first = [&](int end) { return (1u << min(max(end - key0, 0), 16)) - 1u; };  // keys before `end`
+                        s_raw_seen[place][lane] = static_cast<uint16_t>(at != kNoTile ? first(len) & (first(p.sink) | ~first(low)) : 0u);
+                    }
+                    __syncwarp();
                     if (lane == 0) {
                         s_raw_there[place] = there;
                         mbar_arrive_expect_tx(bar, __popc(there) * L::kSubBytes);
@@ -445,7 +453,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
         };
 
         // Codes of a tile in registers: K's of keys g and g + 8 of this warp's 16 (heads of 64: two words of each are used), V's of keys k8 and
-        // k8 + 8 of two parts of 16, and their scales.  V's scales are 0 for keys behind the end or not there, whose bytes may be anything.
+        // k8 + 8 of two parts of 16, and their scales.  V's scales are 0 for keys behind the end, not there or seen by no row, whose bytes may be
+        // anything.
         struct VCodes {
             uint2 c[2][2];
             uint32_t s[2];
@@ -454,7 +463,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
         uint32_t ks = 0;
         unsigned there = 0;
         VCodes v_now, v_one, v_two;  // of the tile just loaded, and of the one and two before
-        auto load = [&](int keys) {  // keys: of the tile, that there are
+        auto load = [&]() {
             const uint32_t place = t % kRawRing;
             wait(bars.raw_full[place], (t / kRawRing) & 1, kTwRaw);
             there = s_raw_there[place];
@@ -476,12 +485,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                 }
                 v_now.s[s2] = ld_shared<uint32_t>(from + 17 * D + (D == 128 ? eighth : eighth >> 1) * 16 + (k8 >> 1) * 4);
             }
-            if (keys < kTile || there != 0xffu) {
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        if ((2 * fw + s2) * 16 + h * 8 + k8 >= keys || !(there >> (2 * fw + s2) & 1)) v_now.s[s2] &= h ? 0x0000ffffu : 0xffff0000u;
+            const uint32_t seen = *reinterpret_cast<const uint32_t*>(&s_raw_seen[place][2 * fw]);
+            if (seen != 0xffffffffu) {
+                const uint32_t bytes = (seen >> k8 & 0x01010101u) * 0xffu;
+                v_now.s[0] &= __byte_perm(bytes, 0u, 0x1100);
+                v_now.s[1] &= __byte_perm(bytes, 0u, 0x3322);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars.raw_free[place]));
@@ -555,7 +563,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
 #pragma unroll 1
         for (int k = 0; same_in_warp(item_ready(k)); ++k) {
             const TileItem& it = s_items[k % kTileItems];
-            const int nt = it.nt, t0 = it.t0, ns = it.ns, skip = it.skip, len = it.len;
+            const int nt = it.nt;
             if (out_k == k) out_end = t + nt;
             started = k + 1;
             // ---- Q: a row a thread, scaled by a power of two to at most 2
@@ -594,8 +602,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars.q_full));
 #pragma unroll 1
-            for (int j = t0; j < t0 + nt; ++j) {
-                load(len - ((j < ns ? j : j + skip) << 7));
+            for (int j = 0; j < nt; ++j) {
+                load();
                 feed_k();
                 if (t > 2) feed_v(v_two);
                 v_two = v_one;

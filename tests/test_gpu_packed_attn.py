@@ -244,6 +244,26 @@ def test_lengths_that_change_between_replays():
         c.k, c.v = k, v
 
 
+@pytest.mark.parametrize("rows,window,sink", [([1, 3], 40, 5), ([2, 1], 100, 0), ([60, 90], 150, 20), ([70, 100], 33, 200)])
+@pytest.mark.parametrize("Hq,Hkv,d", [(7, 1, 128), (4, 1, 64)])
+def test_keys_that_no_row_sees_may_hold_anything(rows, window, sink, Hq, Hkv, d):
+    """Pages between the sink and the window whose bytes are codes of -6 and scales that are NaN (pages given back, say)."""
+    import torch
+    c = Case([700, 900], rows, Hq, Hkv, d, 16, window=window, sink=sink, seed=5)
+    o, lse = c.run()
+    c.check(o, lse)
+    for r, (L, n) in enumerate(zip(c.lens, c.rows)):
+        for t in range(sink, int(L - n - window + 1)):
+            page, u = int(c.table[r, t // 16]), t % 16
+            h, k8, w, g = u // 8, u % 8, d // 64, d // 16
+            tile = c.cache[page, :, 0]
+            # the scales of token u, K's and V's
+            tile[:, [16 * d + k8 * 2 * g + (i // w) * 2 * w + h * w + i % w for i in range(g)]] = 0xFF
+            tile[:, [17 * d + i * 16 + (k8 // 2) * 4 + h * 2 + k8 % 2 for i in range(g)]] = 0xFF
+    o2, lse2 = c.run()
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
 def test_rows_without_lse():
     import torch
     c = Case([100], [2], 4, 2, 64, 16)

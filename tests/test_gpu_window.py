@@ -110,6 +110,26 @@ def test_batches_slack_and_outliers(n, first):
     run(n, first, 64, 0, 4, 2, 64, batch=2, seed=2, with_lse=False)
 
 
+@pytest.mark.parametrize("n,first,window,sink", [(1, 1000, 100, 5), (4, 777, 33, 0), (3, 500, 17, 20), (300, 900, 100, 5), (150, 2000, 130, 60), (40, 1000, 7, 0)])
+@pytest.mark.parametrize("Hq,Hkv,d", [(7, 1, 128), (4, 2, 64)])
+def test_keys_that_no_row_sees_may_hold_anything(n, first, window, sink, Hq, Hkv, d):
+    """A stream that has left its old rows behind: NaN in every key between the sink and the first row's window."""
+    import torch
+    from paper_2506_19651_b200 import binding as pb
+    torch.manual_seed(n)
+    s, keys = pb.make_shape(sink, 1, 0, 1, Hq, Hkv, d), first + n
+    q, k, v = (torch.randn((m, h, d), device="cuda").to(torch.bfloat16) for m, h in ((n, Hq), (keys, Hkv), (keys, Hkv)))
+    ws = torch.zeros(pb.pevlm_window_workspace_bytes(s, window, first, n), dtype=torch.uint8, device="cuda")
+    out = []
+    for _ in range(2):
+        o, lse = torch.zeros_like(q), torch.zeros((Hq, n), device="cuda")
+        pb.pevlm_window_attn(s, window, q, k, v, first, n, keys, o, lse, ws)
+        out.append((o, lse))
+        k[sink:first - window + 1] = float("nan")
+        v[sink:first - window + 1] = float("nan")
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1]) and bool(torch.isfinite(out[1][0]).all())
+
+
 def test_window_of_everything_is_plain_causal():
     """With a window as long as the sequence the rows are those of the full causal prefill, bit for bit."""
     import torch
