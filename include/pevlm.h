@@ -254,7 +254,7 @@ typedef struct {
  * ceil(lens[r] / page_len) pages are pushed onto the free list, and its length becomes 0.
  *   finished, lens [num_seqs], page_table [num_seqs, max_pages], free_count [1]: read
  *   free_list [num_pages]: written from entry *free_count on; lens_out [num_seqs], free_count_out [1]: written
- * Outputs must not be the inputs (PEVLM_EINVAL): a step goes lens -> release -> lens_out -> assign -> lens.  The page table
+ * Outputs must not share memory with inputs (PEVLM_EINVAL): a step goes lens -> release -> lens_out -> assign -> lens.  The page table
  * stays as it is: what stands behind a sequence's length means nothing.  Lengths and counts outside their range count as the
  * nearest one inside; nothing is written past the end of the free list.
  */

@@ -20,11 +20,19 @@ static int check_pages(const pevlm_pages_t* g) {
 
 static int page_shift(const pevlm_pages_t* g) { return __builtin_ctz(static_cast<unsigned>(g->page_len)); }
 
+// Whether two arrays of so many int32 share memory.
+static bool overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + 4 * static_cast<uintptr_t>(m) && y < x + 4 * static_cast<uintptr_t>(n);
+}
+
 // What the packed calls ask of a shape.
 static int check_packed(const pevlm_shape_t* s, const pevlm_pages_t* g) {
     int rc = check_shape(s);
     if (rc == PEVLM_OK) rc = check_pages(g);
     if (rc != PEVLM_OK) return rc;
+    // (the kernels count the cache in 2^32 units of 128 bytes)
+    if (static_cast<double>(g->num_pages) * s->num_kv_heads * (g->page_len / 16) * 18 * s->head_dim >= 128.0 * 4294967295.0) return PEVLM_EUNSUPPORTED;
     return s->batch == 1 ? PEVLM_OK : PEVLM_EUNSUPPORTED;
 }
 
@@ -39,10 +47,11 @@ int pevlm_pages_release(const pevlm_pages_t* g, const int32_t* finished, const i
     int rc = check_pages(g);
     if (rc != PEVLM_OK) return rc;
     if (!finished || !lens || !page_table || !free_list || !free_count || !lens_out || !free_count_out) return PEVLM_EINVAL;
-    if (lens_out == lens || free_count_out == free_count) return PEVLM_EINVAL;
     if (!aligned_to(finished, 4) || !aligned_to(lens, 4) || !aligned_to(page_table, 4) || !aligned_to(free_list, 4) ||
         !aligned_to(free_count, 4) || !aligned_to(lens_out, 4) || !aligned_to(free_count_out, 4))
         return PEVLM_EALIGN;
+    if (overlap(lens_out, g->num_seqs, lens, g->num_seqs) || overlap(lens_out, g->num_seqs, finished, g->num_seqs) || overlap(free_count_out, 1, free_count, 1))
+        return PEVLM_EINVAL;
     rc = check_device();
     if (rc != PEVLM_OK) return rc;
     ReleaseParams p{finished, lens, page_table, free_count, free_list, lens_out, free_count_out, g->num_pages, g->num_seqs, g->max_pages, page_shift(g)};
@@ -58,11 +67,14 @@ int pevlm_pages_assign(const pevlm_pages_t* g, const int32_t* lens, const int32_
     if (max_rows < 0 || max_rows > 1ll << 30) return PEVLM_EINVAL;
     if (!lens || !new_lens || !page_table || !free_list || !free_count || !lens_out || !free_count_out || !row_start) return PEVLM_EINVAL;
     if (max_rows > 0 && (!slots || !positions)) return PEVLM_EINVAL;
-    if (lens_out == lens || lens_out == new_lens || free_count_out == free_count) return PEVLM_EINVAL;
     if (!aligned_to(lens, 4) || !aligned_to(new_lens, 4) || !aligned_to(page_table, 4) || !aligned_to(free_list, 4) ||
         !aligned_to(free_count, 4) || !aligned_to(lens_out, 4) || !aligned_to(free_count_out, 4) || !aligned_to(row_start, 4) ||
         !aligned_to(slots, 16) || !aligned_to(positions, 16))
         return PEVLM_EALIGN;
+    const int64_t n = g->num_seqs;
+    for (const int32_t* in : {lens, new_lens})
+        if (overlap(lens_out, n, in, n) || overlap(row_start, n + 1, in, n) || overlap(slots, max_rows, in, n) || overlap(positions, max_rows, in, n)) return PEVLM_EINVAL;
+    if (overlap(free_count_out, 1, free_count, 1)) return PEVLM_EINVAL;
     rc = check_device();
     if (rc != PEVLM_OK) return rc;
     AssignParams p{lens, new_lens, free_list, free_count, page_table, lens_out, free_count_out, row_start, slots, positions,

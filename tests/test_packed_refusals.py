@@ -55,8 +55,19 @@ def test_pages(lib):
     for out, src in ((5, 0), (5, 1), (6, 4)):
         a = list(assign); a[out] = a[src]
         assert lib.pevlm_pages_assign(C.byref(g), *a, 8, None) == pb.PEVLM_EINVAL
+    for i, other in ((5, 4096 + 12), (7, 4096 + 12), (5, 8192 - 12), (8, 4096), (9, 8192)):  # four lengths at 4096, four more at 8192: parts of them
+        a = list(assign); a[i] = at(other)
+        assert lib.pevlm_pages_assign(C.byref(g), *a, 8, None) == pb.PEVLM_EINVAL, i
+    a = list(release); a[5] = at(4096 + 8)   # finished
+    assert lib.pevlm_pages_release(C.byref(g), *a, None) == pb.PEVLM_EINVAL
     for rows in (-1, 2 ** 30 + 1):
         assert lib.pevlm_pages_assign(C.byref(g), *assign, rows, None) == pb.PEVLM_EINVAL
+
+
+def test_cache_of_more_than_can_be_counted(lib):
+    s, g = pb.make_shape(0, 1, 0, 1, 8, 8, 128), pb.make_pages(2 ** 24, 64, 4, 2)
+    assert pb.pevlm_packed_cache_bytes(s, g) == 0
+    assert pb.pevlm_packed_cache_bytes(s, pb.make_pages(2 ** 21, 64, 4, 2)) == 2 ** 21 * 8 * 4 * 18 * 128
 
 
 def test_packed_rows(lib):
