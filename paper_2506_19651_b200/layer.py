@@ -243,11 +243,24 @@ class PackedCache:
             raise ValueError(f"{', '.join(str(t.shape[0]) for t in tensors)} rows where at most {self.max_rows} fit, the same of each")
         return n
 
+    def _row_stride(self, t, heads):
+        """Elements from one row to the next of rows whose heads stand one after another (the calls get addresses only)."""
+        if t.dtype is not self._q.dtype or t.dim() != 3 or t.shape[1:] != (heads, self.d):
+            raise ValueError(f"rows of {tuple(t.shape)} ({t.dtype}) where bf16 [n, {heads}, {self.d}] is read")
+        if (t.stride(1), t.stride(2)) != (self.d, 1) or (t.shape[0] > 1 and t.stride(0) < heads * self.d):
+            raise ValueError(f"rows with strides {t.stride()}: the {heads} heads of a row have to stand one after another, and rows apart")
+        return t.stride(0) if t.shape[0] > 1 else 0
+
+    def _int_per_sequence(self, t):
+        if t.numel() != self.pages.num_seqs or t.dtype is not self.lens.dtype or not t.is_contiguous():
+            raise ValueError(f"{t.numel()} of {t.dtype} where an int32 for each of {self.pages.num_seqs} sequences is read")
+
     def extend(self, new_lens, finished=None):
         """Gives back the pages of the `finished` sequences and makes room for new_lens (int32, on the GPU, one for each sequence) more tokens
         of each: row_start, slots and positions say where the rows of the step go."""
-        if new_lens.numel() != self.pages.num_seqs or (finished is not None and finished.numel() != self.pages.num_seqs):
-            raise ValueError(f"lengths of {self.pages.num_seqs} sequences")
+        self._int_per_sequence(new_lens)
+        if finished is not None:
+            self._int_per_sequence(finished)
         pb.pevlm_pages_release(self.pages, self._none if finished is None else finished, self.lens, self.page_table, self.free_list,
                                self.free_count, self._lens, self._free_count)
         pb.pevlm_pages_assign(self.pages, self._lens, new_lens, self.page_table, self.free_list, self._free_count, self.lens,
@@ -256,27 +269,35 @@ class PackedCache:
     def store(self, k, v):
         """Rows of roped K and of V [n, Hkv, d] (rows may be strided) into the slots of the last extend()."""
         n = self._rows(k, v)
-        pb.pevlm_packed_store(self.shape, self.pages, k, v, self.slots, n, self.cache, k.stride(0), v.stride(0))
+        pb.pevlm_packed_store(self.shape, self.pages, k, v, self.slots, n, self.cache, self._row_stride(k, self.Hkv), self._row_stride(v, self.Hkv))
 
     def attend(self, q, most=None):
         """Attention of roped q [n, Hq, d], the rows of the last extend().  `most`: rows of one sequence, if the caller knows.
-        Returns (o [n,Hq,d], lse [Hq,n])."""
+        Rows of a sequence that found no room have no meaning.  Returns (o [n,Hq,d], lse [Hq,n])."""
         n = self._rows(q)
+        stride = self._row_stride(q, self.Hq)
         o, lse = q.new_empty((n, self.Hq, self.d)), self._lse.new_empty((self.Hq, n))
         pb.pevlm_packed_attn(self.shape, self.pages, self.window, q, self.cache, self.page_table, self.lens, self.row_start, n,
-                             n if most is None else min(most, n), o, lse, self.workspace, q.stride(0))
+                             n if most is None else min(most, n), o, lse, self.workspace, stride)
         return o, lse
 
     def step(self, q, k, v, new_lens, finished=None, most=None):
         """One step of the layer from un-roped rows: extend(), RoPE at the rows' positions, store(), attend()."""
         n = self._rows(q, k, v)
+        for t, heads in ((q, self.Hq), (k, self.Hkv), (v, self.Hkv)):
+            self._row_stride(t, heads)
+        if not q.is_contiguous() or not k.is_contiguous():
+            raise ValueError("RoPE reads the rows of q and k one after another")
         self.extend(new_lens, finished)
-        pb.pevlm_rope_qk(self.shape, q, k, self._q, self._k, 0, n, self.positions)
+        if n > 0:
+            pb.pevlm_rope_qk(self.shape, q, k, self._q, self._k, 0, n, self.positions)
         self.store(self._k[:n], v)
         return self.attend(self._q[:n], most)
 
     def load(self, slots):
         """K and V [n, Hkv, d] (bf16) as the cache holds them at the given slots (int32, on the GPU)."""
+        if slots.dtype is not self.lens.dtype or not slots.is_contiguous():
+            raise ValueError(f"slots of {slots.dtype} where int32 are read")
         n = slots.numel()
         k, v = (self._k.new_empty((n, self.Hkv, self.d)) for _ in range(2))
         pb.pevlm_packed_load(self.shape, self.pages, self.cache, slots, n, k, v)

@@ -123,6 +123,19 @@ def test_video_encoded_by_blocks_then_asked():
     assert float((o.double() - buf.o_question.double()).norm() / buf.o_question.double().norm()) < 0.35
 
 
+def test_steps_without_rows():
+    """A step that only gives pages back, and one of no rows at all."""
+    import torch
+    from paper_2506_19651_b200.layer import PackedCache
+    c = PackedCache(2, 64, 6, 16, 32, 4, 2, 64, 1e4)
+    rows = lambda n: [torch.randn((n, h, 64), device="cuda").to(torch.bfloat16) for h in (4, 2, 2)]
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    c.step(*rows(20), i32([17, 3]))
+    assert c.lens.tolist() == [17, 3] and int(c.free_count) == 3
+    o, lse = c.step(*rows(0), i32([0, 0]), i32([1, 0]))
+    assert o.shape == (0, 4, 64) and lse.shape == (4, 0) and c.lens.tolist() == [0, 3] and int(c.free_count) == 5
+
+
 def test_captured_decode_loop():
     """Decode steps as one graph that runs on: each replay takes the next token of every sequence."""
     import torch

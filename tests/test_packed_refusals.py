@@ -201,4 +201,18 @@ def test_packed_cache_refuses(monkeypatch):
     with pytest.raises(ValueError, match="2 sequences"):
         c.step(q, k, v, torch.zeros(3, dtype=torch.int32))
     with pytest.raises(ValueError, match="2 sequences"):
+        c.step(q, k, v, torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(ValueError, match="rows apart"):
+        c.store(k, v[:1].expand(4, -1, -1))          # a row for all would be read as four
+    with pytest.raises(ValueError, match="rows apart"):
+        c.attend(q.transpose(0, 1).contiguous().transpose(0, 1))
+    with pytest.raises(ValueError, match="where bf16"):
+        c.attend(q.float())
+    with pytest.raises(ValueError, match="where bf16"):
+        c.store(q, q)
+    with pytest.raises(ValueError, match="one after another"):
+        c.step(torch.zeros(4, 8, 64, dtype=torch.bfloat16)[:, :4], k, v, lens)
+    with pytest.raises(ValueError, match="int32 are read"):
+        c.load(torch.zeros(3, dtype=torch.int64))
+    with pytest.raises(ValueError, match="2 sequences"):
         c.extend(lens, torch.zeros(1, dtype=torch.int32))
