@@ -175,6 +175,11 @@ CASES = {
     "many questions": dict(lens=[(i * 53) % 400 for i in range(150)], rows=[(i * 7) % 60 for i in range(150)], Hq=4, Hkv=2, d=64, P=16),
     "question, large keys": dict(lens=[600], rows=[64], Hq=7, Hkv=1, d=128, P=16, k_scale=8.0),
     "question, small and strided queries": dict(lens=[500], rows=[64], Hq=4, Hkv=1, d=64, P=16, q_scale=2.0 ** -90, k_scale=20.0, stride=4 * 64 + 128, extra_rows=3),
+    "group of 40": dict(lens=[200, 31, 0], rows=[1, 1, 1], Hq=40, Hkv=1, d=64, P=16),
+    "group of 128": dict(lens=[300, 31, 0, 129], rows=[1, 2, 1, 1], Hq=128, Hkv=1, d=128, P=16),
+    "128 heads on 128": dict(lens=[70, 200], rows=[1, 2], Hq=128, Hkv=128, d=64, P=16),
+    "many under a window": dict(lens=[(i * 37) % 700 for i in range(300)], rows=[1 + i % 2 for i in range(300)], Hq=4, Hkv=1, d=64, P=32, window=50, sink=4),
+    "many questions under a window": dict(lens=[(i * 53) % 700 for i in range(200)], rows=[(i * 7) % 60 for i in range(200)], Hq=4, Hkv=2, d=64, P=16, window=90, sink=20),
     "scale": dict(lens=[100], rows=[1], Hq=4, Hkv=2, d=64, P=16, scale=0.5),
 }
 
@@ -262,6 +267,41 @@ def test_keys_that_no_row_sees_may_hold_anything(rows, window, sink, Hq, Hkv, d)
             tile[:, [17 * d + i * 16 + (k8 // 2) * 4 + h * 2 + k8 % 2 for i in range(g)]] = 0xFF
     o2, lse2 = c.run()
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("rows", [[2, 3], [3, 5], [64, 100]])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_row_that_is_no_number_stays_alone(rows, value):
+    c = Case([500, 333], rows, 6, 2, 64, 16, seed=7)
+    o, lse = c.run()
+    at = rows[0] + 1  # the second row of the second sequence, one of its heads
+    c.q[at, 64:128] = value
+    o2, lse2 = c.run()
+    if value != value:
+        assert bool(o2[at, 1].isnan().all())
+    o2[at, 1], lse2[1, at] = o[at, 1], lse[1, at]
+    c.check(o2, lse2)
+
+
+def test_calls_on_two_streams_at_once():
+    """Each with its own workspace; both kernels take every SM."""
+    import torch
+    cases = [Case([9000, 40], [1, 2], 8, 2, 128, 64, seed=1), Case([3000], [200], 8, 2, 64, 16, seed=2)]
+    calls, streams, got = [], [torch.cuda.Stream(), torch.cuda.Stream()], []
+    want = [c.run() for c in cases]
+    for c in cases:
+        most = int(c.rows.max())
+        ws = torch.empty(c.pb.pevlm_packed_workspace_bytes(c.shape, c.pages, c.n_rows, most), dtype=torch.uint8, device="cuda")
+        calls.append((c, most, ws, torch.zeros((c.n_rows, c.Hq, c.d), dtype=torch.bfloat16, device="cuda"), torch.zeros((c.Hq, c.n_rows), device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, (c, most, ws, o, lse) in zip(streams, calls):
+            with torch.cuda.stream(stream):
+                c.pb.pevlm_packed_attn(c.shape, c.pages, 0, c.q, c.cache, c.table, c.d_lens, c.start, c.n_rows, most, o, lse, ws)
+    torch.cuda.synchronize()
+    for (o, lse), (_, _, ws, o2, lse2) in zip(want, calls):
+        assert cases[0].pb.pevlm_read_status(ws) == (0, 0)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
 def test_rows_without_lse():

@@ -143,3 +143,22 @@ def test_infinities_and_nan_leave_numbers():
     ko, vo = torch.empty_like(k), torch.empty_like(k)
     pb.pevlm_packed_load(s, g, cache, slots, 16, ko, vo)
     assert bool(torch.isfinite(ko).all()) and bool(torch.isfinite(vo).all())
+
+
+def test_the_same_slot_again_and_again():
+    """One slot in every row that is read, and the last bytes of a cache that ends there."""
+    import torch
+    from paper_2506_19651_b200 import binding as pb
+    s, g = pb.make_shape(0, 1, 0, 1, 2, 2, 128), pb.make_pages(3, 16, 1, 3)
+    cache = GuardedAllocator()((3, 2, 1, 18 * 128), torch.uint8)
+    cache.fill_(0)
+    k, v = (torch.randn((48, 2, 128), device="cuda").to(torch.bfloat16) for _ in range(2))
+    pb.pevlm_packed_store(s, g, k, v, torch.arange(48, dtype=torch.int32, device="cuda"), 48, cache)
+    for slot in (0, 17, 47):
+        once, many = ([torch.empty((n, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)] for n in (1, 5000))
+        pb.pevlm_packed_load(s, g, cache, torch.tensor([slot], dtype=torch.int32, device="cuda"), 1, *once)
+        pb.pevlm_packed_load(s, g, cache, torch.full((5000,), slot, dtype=torch.int32, device="cuda"), 5000, *many)
+        for a, b in zip(once, many):
+            assert bool((a == b).all())
+        for a, x in zip(once, (k, v)):
+            assert np.array_equal(_values(a)[0], R.dequantise(*R.quantise(_values(x[slot:slot + 1])))[0])

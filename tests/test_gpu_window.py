@@ -130,6 +130,26 @@ def test_keys_that_no_row_sees_may_hold_anything(n, first, window, sink, Hq, Hkv
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1]) and bool(torch.isfinite(out[1][0]).all())
 
 
+@pytest.mark.parametrize("n,first", [(3, 400), (200, 400)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_row_that_is_no_number_stays_alone(n, first, value):
+    import torch
+    from paper_2506_19651_b200 import binding as pb
+    torch.manual_seed(n)
+    Hq, Hkv, d, window, sink = 6, 2, 64, 100, 5
+    s, keys = pb.make_shape(sink, 1, 0, 1, Hq, Hkv, d), first + n
+    q, k, v = (torch.randn((m, h, d), device="cuda").to(torch.bfloat16) for m, h in ((n, Hq), (keys, Hkv), (keys, Hkv)))
+    ws = torch.zeros(pb.pevlm_window_workspace_bytes(s, window, first, n), dtype=torch.uint8, device="cuda")
+    want, z, tol, tol_z = definition(_values(q), _values(k), _values(v), first, window, sink, d ** -0.5)
+    q[1, 4] = value
+    o, lse = torch.zeros_like(q), torch.zeros((Hq, n), device="cuda")
+    pb.pevlm_window_attn(s, window, q, k, v, first, n, keys, o, lse, ws)
+    others = np.ones((n, Hq), bool)
+    others[1, 4] = False
+    got, got_z = _values(o), lse.double().cpu().numpy().T
+    assert (np.abs(got - want) <= tol)[others].all() and (np.abs(got_z - z) <= tol_z)[others].all()
+
+
 def test_window_of_everything_is_plain_causal():
     """With a window as long as the sequence the rows are those of the full causal prefill, bit for bit."""
     import torch
