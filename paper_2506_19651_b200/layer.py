@@ -213,7 +213,7 @@ class PackedCache:
     GPU, so a step may be captured into a graph and replayed with whatever `new_lens` and `finished` hold by then.
 
     `max_rows` rows at most a step, of all sequences one after another; `window` > 0 leaves each row the last `window` positions and its
-    sequence's first `sink` ones.  A sequence that finds no pages keeps its length and its rows get slot -1 (see pevlm_pages_assign)."""
+    sequence's first `sink` ones.  Steps follow one another on one stream: the workspace and the roped rows are the object's.  A sequence that finds no pages keeps its length and its rows get slot -1 (see pevlm_pages_assign)."""
 
     def __init__(self, num_seqs, max_tokens, num_pages, page_len, max_rows, Hq, Hkv, d, theta, window=0, sink=0, scale=0.0, device="cuda"):
         import torch
@@ -243,24 +243,34 @@ class PackedCache:
             raise ValueError(f"{', '.join(str(t.shape[0]) for t in tensors)} rows where at most {self.max_rows} fit, the same of each")
         return n
 
+    def _at_hand(self, *tensors):
+        """The calls go to the current device and take addresses: all of it has to be there."""
+        import torch
+        at = self.cache.device
+        if at.type != "cuda" or at.index != torch.cuda.current_device():
+            raise ValueError(f"a cache on {at}, which is not the current device")
+        for t in tensors:
+            if t is not None and t.device != at:
+                raise ValueError(f"a tensor on {t.device} beside a cache on {at}")
+
     def _row_stride(self, t, heads):
         """Elements from one row to the next of rows whose heads stand one after another (the calls get addresses only)."""
         if t.dtype is not self._q.dtype or t.dim() != 3 or t.shape[1:] != (heads, self.d):
             raise ValueError(f"rows of {tuple(t.shape)} ({t.dtype}) where bf16 [n, {heads}, {self.d}] is read")
-        if (t.stride(1), t.stride(2)) != (self.d, 1) or (t.shape[0] > 1 and t.stride(0) < heads * self.d):
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.d) or (t.shape[0] > 1 and t.stride(0) < heads * self.d):
             raise ValueError(f"rows with strides {t.stride()}: the {heads} heads of a row have to stand one after another, and rows apart")
         return t.stride(0) if t.shape[0] > 1 else 0
 
-    def _int_per_sequence(self, t):
-        if t.numel() != self.pages.num_seqs or t.dtype is not self.lens.dtype or not t.is_contiguous():
-            raise ValueError(f"{t.numel()} of {t.dtype} where an int32 for each of {self.pages.num_seqs} sequences is read")
+    def _int_per_sequence(self, *tensors):
+        for t in tensors:
+            if t is not None and (t.numel() != self.pages.num_seqs or t.dtype is not self.lens.dtype or not t.is_contiguous()):
+                raise ValueError(f"{t.numel()} of {t.dtype} where an int32 for each of {self.pages.num_seqs} sequences is read")
 
     def extend(self, new_lens, finished=None):
         """Gives back the pages of the `finished` sequences and makes room for new_lens (int32, on the GPU, one for each sequence) more tokens
         of each: row_start, slots and positions say where the rows of the step go."""
-        self._int_per_sequence(new_lens)
-        if finished is not None:
-            self._int_per_sequence(finished)
+        self._int_per_sequence(new_lens, finished)
+        self._at_hand(new_lens, finished)
         pb.pevlm_pages_release(self.pages, self._none if finished is None else finished, self.lens, self.page_table, self.free_list,
                                self.free_count, self._lens, self._free_count)
         pb.pevlm_pages_assign(self.pages, self._lens, new_lens, self.page_table, self.free_list, self._free_count, self.lens,
@@ -269,13 +279,16 @@ class PackedCache:
     def store(self, k, v):
         """Rows of roped K and of V [n, Hkv, d] (rows may be strided) into the slots of the last extend()."""
         n = self._rows(k, v)
-        pb.pevlm_packed_store(self.shape, self.pages, k, v, self.slots, n, self.cache, self._row_stride(k, self.Hkv), self._row_stride(v, self.Hkv))
+        strides = self._row_stride(k, self.Hkv), self._row_stride(v, self.Hkv)
+        self._at_hand(k, v)
+        pb.pevlm_packed_store(self.shape, self.pages, k, v, self.slots, n, self.cache, *strides)
 
     def attend(self, q, most=None):
         """Attention of roped q [n, Hq, d], the rows of the last extend().  `most`: rows of one sequence, if the caller knows.
         Rows of a sequence that found no room have no meaning.  Returns (o [n,Hq,d], lse [Hq,n])."""
         n = self._rows(q)
         stride = self._row_stride(q, self.Hq)
+        self._at_hand(q)
         o, lse = q.new_empty((n, self.Hq, self.d)), self._lse.new_empty((self.Hq, n))
         pb.pevlm_packed_attn(self.shape, self.pages, self.window, q, self.cache, self.page_table, self.lens, self.row_start, n,
                              n if most is None else min(most, n), o, lse, self.workspace, stride)
@@ -288,6 +301,8 @@ class PackedCache:
             self._row_stride(t, heads)
         if not q.is_contiguous() or not k.is_contiguous():
             raise ValueError("RoPE reads the rows of q and k one after another")
+        self._int_per_sequence(new_lens, finished)
+        self._at_hand(q, k, v)
         self.extend(new_lens, finished)
         if n > 0:
             pb.pevlm_rope_qk(self.shape, q, k, self._q, self._k, 0, n, self.positions)
@@ -298,6 +313,7 @@ class PackedCache:
         """K and V [n, Hkv, d] (bf16) as the cache holds them at the given slots (int32, on the GPU)."""
         if slots.dtype is not self.lens.dtype or not slots.is_contiguous():
             raise ValueError(f"slots of {slots.dtype} where int32 are read")
+        self._at_hand(slots)
         n = slots.numel()
         k, v = (self._k.new_empty((n, self.Hkv, self.d)) for _ in range(2))
         pb.pevlm_packed_load(self.shape, self.pages, self.cache, slots, n, k, v)

@@ -216,3 +216,14 @@ def test_packed_cache_refuses(monkeypatch):
         c.load(torch.zeros(3, dtype=torch.int64))
     with pytest.raises(ValueError, match="2 sequences"):
         c.extend(lens, torch.zeros(1, dtype=torch.int32))
+    # a cache, or a tensor beside it, that the current device does not have
+    for call in (lambda: c.extend(lens), lambda: c.store(k, v), lambda: c.attend(q), lambda: c.step(q, k, v, lens), lambda: c.load(lens)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    class Elsewhere:
+        device = torch.device("cuda", 1)
+    c.cache = Elsewhere()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: c.extend(lens), lambda: c.store(k, v), lambda: c.attend(q), lambda: c.step(q, k, v, lens), lambda: c.load(lens)):
+        with pytest.raises(ValueError, match="on cpu beside"):
+            call()
