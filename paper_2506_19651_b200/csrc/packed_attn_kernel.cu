@@ -181,11 +181,16 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
         // first 32 of the next unit (`after`), so that a page is looked up long before it is needed.
         int at;
         PackedUnit<4> cur(part, at), after(cur);
-        after.next(p, L::kRows, table);
         // Places [from, from + kUnitTiles<4>) of the list belong to a unit, its tiles follow.  Those of it that are in the part:
         int64_t unit0 = lo - at + kUnitTiles<4>;  // of the unit's first tile
         int first_tile = max(at - kUnitTiles<4>, 0);
         auto tiles_of = [&](const PackedUnit<4>& u, int64_t tile0) { return static_cast<int>(max(min(hi - tile0, static_cast<int64_t>(u.s.cnt)), static_cast<int64_t>(0))); };
+        // (a unit that the part does not reach is not looked for)
+        auto to_next = [&](PackedUnit<4>& u, int64_t tile0) {
+            if (tile0 < hi) u.next(p, L::kRows, table);
+            else u.r = p.num_seqs;
+        };
+        to_next(after, unit0 + cur.s.cnt + kUnitTiles<4>);
         int64_t fetch0 = unit0;                          // the same of the unit that is fetched
         int left = tiles_of(cur, fetch0) - first_tile;   // and its tiles that are yet to be
         int in_block = 0, block = first_tile;            // of 32 places, and their first tile
@@ -283,7 +288,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                         in_block = block = 0;
                         places = place_of(ahead, lane, page_after);
                         page_next = page_of(ahead, 32 + lane);
-                        after.next(p, L::kRows, table);
+                        to_next(after, fetch0 + ahead.s.cnt + kUnitTiles<4>);
                         page_after = page_of(after, lane);
                         prefetch_rows(ahead);
                     }
@@ -519,7 +524,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
             unit0 += cur.s.cnt + kUnitTiles<4>;
             first_unit = false;
             first_tile = 0;
-            cur.next(p, L::kRows, table);
+            to_next(cur, unit0);
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
     }

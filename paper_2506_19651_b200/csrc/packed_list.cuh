@@ -92,6 +92,29 @@ struct PackedPart {
     PackedSeq s;  // that sequence
 };
 
+// First sequence from r on that has rows (num_seqs: none has), for a whole warp: 128 are looked at together, since a server's table may hold many
+// that have none in this call.
+__device__ __forceinline__ int seq_with_rows(const PackedAttnParams& p, int r) {
+    const int lane = threadIdx.x & 31;
+    for (; r < p.num_seqs; r += 128) {
+        int from[4], to[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int x = min(r + 32 * i + lane, p.num_seqs - 1);
+            from[i] = p.row_start[x];
+            to[i] = p.row_start[x + 1];
+        }
+        int found = p.num_seqs;
+#pragma unroll
+        for (int i = 3; i >= 0; --i) {
+            const unsigned some = __ballot_sync(0xffffffffu, r + 32 * i + lane < p.num_seqs && min(to[i], p.n_rows) > max(from[i], 0));
+            if (some != 0) found = r + 32 * i + __ffs(some) - 1;
+        }
+        if (found < p.num_seqs) return found;
+    }
+    return p.num_seqs;
+}
+
 // A unit on the list.
 template <int TS>
 struct PackedUnit {
@@ -104,16 +127,17 @@ struct PackedUnit {
         head = static_cast<int>(divided(unit, s.chunks));
         chunk = static_cast<int>(unit - static_cast<int64_t>(head) * s.chunks);
     }
-    // The next one; past the last, r = num_seqs.  `table`: the sequences' descriptions in shared memory, or NULL.
+    // The next one, for a whole warp; past the last, r = num_seqs.  `table`: the sequences' descriptions in shared memory, or NULL.
     __device__ __forceinline__ void next(const PackedAttnParams& p, int rows_per_chunk, const PackedSeq* table) {
         if (++chunk < s.chunks) return;
         chunk = 0;
         if (++head < p.Hkv) return;
         head = 0;
-        do {
-            if (++r >= p.num_seqs) return;
-            s = table ? table[r] : packed_seq<TS>(p, r, rows_per_chunk);
-        } while (s.chunks == 0);
+        if (++r >= p.num_seqs) return;
+        s = table ? table[r] : packed_seq<TS>(p, r, rows_per_chunk);
+        if (s.chunks > 0) return;
+        r = seq_with_rows(p, r + 1);
+        if (r < p.num_seqs) s = table ? table[r] : packed_seq<TS>(p, r, rows_per_chunk);
     }
     __device__ __forceinline__ int key0(int x) const { return (x < s.ns ? x : x + s.skip) << TS; }
     // Tiles [from, to) of the unit, of whose keys every row at positions pos_min .. pos_max sees all.

@@ -105,25 +105,38 @@ __device__ __forceinline__ int same_in_warp(int x) { return __shfl_sync(0xffffff
 __device__ __forceinline__ void turn_wait(int what, int wg, int quarter) { asm volatile("bar.sync %0, 64;" ::"r"(what + wg * 4 + quarter) : "memory"); }
 __device__ __forceinline__ void turn_pass(int what, int wg, int quarter) { asm volatile("bar.arrive %0, 64;" ::"r"(what + (wg ^ 1) * 4 + quarter) : "memory"); }
 
-// Worker `me` of the list, by one warp: its part.
+// Worker `me` of the list, by one warp: its part.  A lane has four neighbouring sequences at a time.
 __device__ __forceinline__ PackedPart part_by_warp(const PackedAttnParams& p, int rows_per_chunk, int me, int workers) {
     const int lane = threadIdx.x & 31;
     auto tiles_of = [&](int r) { return r < p.num_seqs ? seq_tiles<7>(p, packed_seq<7>(p, r, rows_per_chunk)) : 0; };
     int64_t total = 0;
-    for (int r0 = 0; r0 < p.num_seqs; r0 += 32) total += tiles_of(r0 + lane);
+    for (int r0 = 4 * lane; r0 < p.num_seqs; r0 += 128) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) total += tiles_of(r0 + i);
+    }
 #pragma unroll
     for (int by = 16; by > 0; by /= 2) total += __shfl_xor_sync(0xffffffffu, total, by);
     PackedPart part{PackedDeal(total, workers), 0, 0, {}};
     const int64_t lo = part.deal.start(me);
     if (lo >= part.deal.start(me + 1)) return part;
     int64_t base = 0;
-    for (int r0 = 0; r0 < p.num_seqs; r0 += 32) {
-        const int64_t mine = tiles_of(r0 + lane), to = base + warp_inclusive(mine);
+    for (int r0 = 0; r0 < p.num_seqs; r0 += 128) {
+        const int r = r0 + 4 * lane;
+        int64_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine += tiles_of(r + i);
+        const int64_t to = base + warp_inclusive(mine);
         const unsigned past = __ballot_sync(0xffffffffu, to > lo);
         if (past) {
             const int l = __ffs(past) - 1;
-            part.seq = r0 + l;
+            part.seq = r0 + 4 * l;
             part.off = lo - __shfl_sync(0xffffffffu, to - mine, l);
+            for (int i = 0; i < 3; ++i) {
+                const int64_t of_seq = tiles_of(part.seq);
+                if (part.off < of_seq) break;
+                part.off -= of_seq;
+                ++part.seq;
+            }
             part.s = packed_seq<7>(p, part.seq, rows_per_chunk);
             break;
         }

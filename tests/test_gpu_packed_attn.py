@@ -180,6 +180,10 @@ CASES = {
     "128 heads on 128": dict(lens=[70, 200], rows=[1, 2], Hq=128, Hkv=128, d=64, P=16),
     "many under a window": dict(lens=[(i * 37) % 700 for i in range(300)], rows=[1 + i % 2 for i in range(300)], Hq=4, Hkv=1, d=64, P=32, window=50, sink=4),
     "many questions under a window": dict(lens=[(i * 53) % 700 for i in range(200)], rows=[(i * 7) % 60 for i in range(200)], Hq=4, Hkv=2, d=64, P=16, window=90, sink=20),
+    "one of many": dict(lens=[0] * 700 + [900] + [40] * 200, rows=[0] * 700 + [2] + [0] * 200, Hq=8, Hkv=2, d=64, P=16),
+    "few of many": dict(lens=[(i * 31) % 500 for i in range(1500)], rows=[i % 3 + 1 if i in (0, 1, 129, 130, 700, 1403, 1499) else 0 for i in range(1500)], Hq=4, Hkv=2, d=128, P=32),
+    "questions of a few of many": dict(lens=[(i * 31) % 500 for i in range(1500)], rows=[i % 100 + 1 if i in (0, 1, 2, 3, 4, 129, 130, 700, 1403, 1499) else 0 for i in range(1500)], Hq=4, Hkv=2, d=64, P=16),
+    "few of 128": dict(lens=[200] * 128, rows=[2 if i in (5, 6, 90, 127) else 0 for i in range(128)], Hq=4, Hkv=2, d=64, P=16),
     "scale": dict(lens=[100], rows=[1], Hq=4, Hkv=2, d=64, P=16, scale=0.5),
 }
 
