@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 // 2^e <= top < 2^(e + 1); down by 2^e, the softmax scale up by it
                 const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23), 1), 253);
-                const float down = __uint_as_float(static_cast<uint32_t>(254 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(e) << 23) * p.scale_log2;
+                const float down = __uint_as_float(static_cast<uint32_t>(254 - e) << 23), up = row_scale(e, p.scale_log2);
 #pragma unroll
                 for (int c = 0; c < KS * 2; ++c)
                     q[j][c >> 1][c & 1] = pack_f16x2(__uint_as_float(x[c] << 16) * down, __uint_as_float(x[c] & 0xffff0000u) * down);

@@ -92,6 +92,12 @@ struct PackedPart {
     PackedSeq s;  // that sequence
 };
 
+// Softmax scale, in units of log2, of a row of Q that is held 2^(e - 127) times smaller.  Kept within the normal numbers: the scores it goes with
+// are below 2^21, which makes nothing of the smallest, but -inf of a hidden key times 0 would be no number.
+__device__ __forceinline__ float row_scale(int e, float scale_log2) {
+    return fminf(fmaxf(__uint_as_float(static_cast<uint32_t>(e) << 23) * scale_log2, 1.17549435e-38f), 3.40282347e38f);
+}
+
 // First sequence from r on that has rows (num_seqs: none has), for a whole warp: 128 are looked at together, since a server's table may hold many
 // that have none in this call.
 __device__ __forceinline__ int seq_with_rows(const PackedAttnParams& p, int r) {

@@ -599,7 +599,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                 const float top = fmaxf(__uint_as_float(top2 << 16), __uint_as_float(top2 & 0xffff0000u));
                 const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23), 1), 253);
                 const float down = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
-                s_scale[k & 3][row] = __uint_as_float(static_cast<uint32_t>(e) << 23) * p.scale_log2;
+                s_scale[k & 3][row] = row_scale(e, p.scale_log2);
 #pragma unroll 4
                 for (int c = 0; c < D / 8; ++c) {
                     const uint4 x = some ? src[c] : make_uint4(0u, 0u, 0u, 0u);

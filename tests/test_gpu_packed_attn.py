@@ -308,6 +308,17 @@ def test_calls_on_two_streams_at_once():
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("rows", [1, 70])
+def test_no_query_and_the_smallest_scale(rows):
+    """Rows of Q that are 0 weigh all that they see alike, and so does a scale that leaves nothing of the scores."""
+    c = Case([100, 60], [rows, 2], 4, 2, 64, 16, scale=2.0 ** -40, seed=6)
+    c.q.view(-1)[:64] = 0
+    c.q_values = _values(c.q)[:c.used].reshape(c.used, 4, 64)
+    c.check(*c.run())
+    c = Case([100, 60], [rows, 2], 4, 2, 64, 16, q_scale=2.0 ** -120, scale=2.0 ** -30, seed=6)
+    c.check(*c.run())
+
+
 def test_rows_without_lse():
     import torch
     c = Case([100], [2], 4, 2, 64, 16)
