@@ -315,7 +315,8 @@ int pevlm_packed_load(const pevlm_shape_t* shape, const pevlm_pages_t* pages, co
  * only those of the last `window` positions (its own among them) and of the sequence's first sink_len tokens (shape); window = 0: all.
  *   q [n_rows, Hq, d] bf16 roped, rows q_stride elements apart (0 = Hq * d); lens [num_seqs], row_start [num_seqs + 1], page_table: as
  *   pevlm_pages_assign leaves them;  o [n_rows, Hq, d] bf16, lse [Hq, n_rows] fp32 (may be NULL), written
- *   max_rows: most rows of one sequence, as the caller knows it (n_rows if not): chooses the kernel, a larger row count stays correct
+ *   max_rows: most rows of one sequence, as the caller knows it (n_rows if not): chooses the kernels, which takes time if it is far too large; a larger
+ *   row count than that stays correct
  * A row that sees no key (a length of 0, or fewer keys than rows) has output 0 and LSE -inf.  Keys in a page whose table entry is outside
  * [0, num_pages) count as not there, and what keys hold that no row sees (behind the length, in front of the windows) does not matter.  Rows of q that no sequence has are not read, and of o and lse not written.  Scores of finite rows are formed from fp16
  * operands (the cache's values are exact in it) and summed in fp32, probabilities rounded to fp16.

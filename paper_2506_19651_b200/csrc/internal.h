@@ -255,12 +255,13 @@ struct PackedAttnParams {
     int32_t n_rows, num_seqs, num_pages, max_pages, page_shift;
     int32_t Hq, Hkv, G;
     int32_t window, sink;    // window = 0: none
+    int32_t n_from, n_to;    // row counts of the sequences that this launch serves
     Divisor div_g;
     float scale_log2;        // softmax scale * log2(e)
 };
-// `rows`: most rows of one sequence and kv head; few of them go to packed_attn_kernel, more to packed_tile_kernel.
-size_t packed_attn_workspace_bytes(int head_dim, int64_t rows);
-cudaError_t launch_packed_attn(const PackedAttnParams& p, int head_dim, int64_t rows, cudaStream_t stream);
+// `max_rows`: most rows of one sequence, as far as the host knows.  Few of a kv head go to packed_attn_kernel, more to packed_tile_kernel.
+size_t packed_attn_workspace_bytes(int head_dim, int64_t rows);  // rows: of a kv head
+cudaError_t launch_packed_attn(PackedAttnParams p, int head_dim, int64_t max_rows, cudaStream_t stream);
 cudaError_t launch_packed_tile(const PackedAttnParams& p, int head_dim, cudaStream_t stream);  // without its merge
 
 cudaError_t launch_rope(const RopeParams& p, int head_dim, cudaStream_t stream);

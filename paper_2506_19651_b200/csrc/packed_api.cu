@@ -164,7 +164,7 @@ int pevlm_packed_attn(const pevlm_shape_t* s, const pevlm_pages_t* g, int32_t wi
         return PEVLM_EALIGN;
     if (!workspace || workspace_bytes < pevlm_packed_workspace_bytes(s, g, n_rows, max_rows)) return PEVLM_EWORKSPACE;
     if (!aligned_to(workspace, 256)) return PEVLM_EALIGN;
-    if (n_rows == 0 || max_rows == 0) return PEVLM_OK;
+    if (n_rows == 0) return PEVLM_OK;
     rc = check_device();
     if (rc != PEVLM_OK) return rc;
     PackedAttnParams p;
@@ -185,7 +185,7 @@ int pevlm_packed_attn(const pevlm_shape_t* s, const pevlm_pages_t* g, int32_t wi
     p.sink = s->sink_len;
     p.div_g = make_divisor(p.G);
     p.scale_log2 = resolve_scale(s) * 1.4426950408889634f;
-    const cudaError_t e = launch_packed_attn(p, s->head_dim, max_rows * p.G, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_packed_attn(p, s->head_dim, max_rows, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? PEVLM_OK : cuda_fail(e, "packed attention launch");
 }
 

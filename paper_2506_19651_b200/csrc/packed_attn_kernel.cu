@@ -679,17 +679,35 @@ static cudaError_t launch_tiles(const PackedAttnParams& p, cudaStream_t stream) 
 // Measured, few rows against tiles: 28/4 heads of 128, 50K keys 28 rows 29.7 / 34.6 us, 35 rows 36.6 / 34.7, 56 rows 43.6 / 35.9; 64 sequences of
 // 1 to 4K keys 28 rows 72.0 / 91.5, 35 rows 94.7 / 91.7.  32/8 heads of 64, 50K keys 48 rows 41.1 / 48.0, 64 rows 49.9 / 48.2; 64 sequences
 // 48 rows 115 / 144, 64 rows 143 / 146.
-static bool takes_tiles(int64_t rows, int head_dim) { return rows > (head_dim == 128 ? 32 : 48); }
+static int most_few(int head_dim) { return head_dim == 128 ? 32 : 48; }
+static bool takes_tiles(int64_t rows, int head_dim) { return rows > most_few(head_dim); }
 
 size_t packed_attn_workspace_bytes(int head_dim, int64_t rows) {
     const int unit = takes_tiles(rows, head_dim) ? kTile : 16;  // rows for each CTA
     return sizeof(PackedJoin) * kNumSms + 2 * static_cast<size_t>(kNumSms) * unit * (head_dim + 2) * sizeof(float);
 }
 
-cudaError_t launch_packed_attn(const PackedAttnParams& p, int head_dim, int64_t rows, cudaStream_t stream) {
-    if (takes_tiles(rows, head_dim)) return head_dim == 128 ? launch_tiles<128>(p, stream) : launch_tiles<64>(p, stream);
+static cudaError_t launch_few(const PackedAttnParams& p, int head_dim, int64_t rows, cudaStream_t stream) {
     if (head_dim == 128) return rows > 8 ? launch_rows<128, 2>(p, stream) : launch_rows<128, 1>(p, stream);
     return rows > 8 ? launch_rows<64, 2>(p, stream) : launch_rows<64, 1>(p, stream);
+}
+
+cudaError_t launch_packed_attn(PackedAttnParams p, int head_dim, int64_t max_rows, cudaStream_t stream) {
+    p.n_from = 1;
+    p.n_to = INT32_MAX;
+    if (!takes_tiles(max_rows * p.G, head_dim)) return launch_few(p, head_dim, max_rows * p.G, stream);
+    // Sequences with few rows beside some with many, or a caller who does not know: a launch for either kind, unless n_rows can only be so
+    // many if all have more than a few.  64 sequences of 4K keys (28/4 heads of 128): 63 single tokens beside a question of 64 137 -> 80 us, 64
+    // single tokens that are said to be up to 64 rows 129 -> 61 (40 if said to be one); launches without work take 12.
+    const int few = most_few(head_dim) / p.G;  // rows of a sequence that are not worth a tile
+    if (few > 0 && p.n_rows <= (p.num_seqs - 1) * max_rows + few) {
+        p.n_to = few;
+        const cudaError_t e = launch_few(p, head_dim, few * p.G, stream);
+        if (e != cudaSuccess) return e;
+        p.n_from = few + 1;
+        p.n_to = INT32_MAX;
+    }
+    return head_dim == 128 ? launch_tiles<128>(p, stream) : launch_tiles<64>(p, stream);
 }
 
 }  // namespace pevlm

@@ -29,6 +29,7 @@ __device__ __forceinline__ PackedSeq packed_seq(const PackedAttnParams& p, int l
     s.len = min(max(len, 0), p.max_pages << p.page_shift);
     s.row0 = min(max(from, 0), p.n_rows);
     s.n = max(min(to, p.n_rows) - s.row0, 0);
+    if (s.n < p.n_from || s.n > p.n_to) s.n = 0;
     s.chunks = (s.n * p.G + rows_per_chunk - 1) / rows_per_chunk;
     s.ns = s.skip = 0;
     constexpr int kKeys = 1 << TS;
@@ -113,7 +114,8 @@ __device__ __forceinline__ int seq_with_rows(const PackedAttnParams& p, int r) {
         int found = p.num_seqs;
 #pragma unroll
         for (int i = 3; i >= 0; --i) {
-            const unsigned some = __ballot_sync(0xffffffffu, r + 32 * i + lane < p.num_seqs && min(to[i], p.n_rows) > max(from[i], 0));
+            const int n = min(to[i], p.n_rows) - max(from[i], 0);
+            const unsigned some = __ballot_sync(0xffffffffu, r + 32 * i + lane < p.num_seqs && n > 0 && n >= p.n_from && n <= p.n_to);
             if (some != 0) found = r + 32 * i + __ffs(some) - 1;
         }
         if (found < p.num_seqs) return found;

@@ -284,7 +284,7 @@ class PackedCache:
         pb.pevlm_packed_store(self.shape, self.pages, k, v, self.slots, n, self.cache, *strides)
 
     def attend(self, q, most=None):
-        """Attention of roped q [n, Hq, d], the rows of the last extend().  `most`: rows of one sequence, if the caller knows.
+        """Attention of roped q [n, Hq, d], the rows of the last extend().  `most`: rows of one sequence, if the caller knows (saves two launches).
         Rows of a sequence that found no room have no meaning.  Returns (o [n,Hq,d], lse [Hq,n])."""
         n = self._rows(q)
         stride = self._row_stride(q, self.Hq)

@@ -184,6 +184,9 @@ CASES = {
     "few of many": dict(lens=[(i * 31) % 500 for i in range(1500)], rows=[i % 3 + 1 if i in (0, 1, 129, 130, 700, 1403, 1499) else 0 for i in range(1500)], Hq=4, Hkv=2, d=128, P=32),
     "questions of a few of many": dict(lens=[(i * 31) % 500 for i in range(1500)], rows=[i % 100 + 1 if i in (0, 1, 2, 3, 4, 129, 130, 700, 1403, 1499) else 0 for i in range(1500)], Hq=4, Hkv=2, d=64, P=16),
     "few of 128": dict(lens=[200] * 128, rows=[2 if i in (5, 6, 90, 127) else 0 for i in range(128)], Hq=4, Hkv=2, d=64, P=16),
+    "single tokens beside a question": dict(lens=[300 + i for i in range(40)], rows=[1] * 20 + [70] + [1] * 18 + [5], Hq=7, Hkv=1, d=128, P=32),
+    "single tokens beside a question, heads of 64": dict(lens=[300 + i for i in range(40)], rows=[2] * 30 + [33] + [0] * 8 + [90], Hq=8, Hkv=2, d=64, P=16, window=200, sink=9),
+    "rows of no sequence": dict(lens=[300, 20, 0], rows=[0, 0, 0], Hq=4, Hkv=2, d=64, P=16, extra_rows=40),
     "scale": dict(lens=[100], rows=[1], Hq=4, Hkv=2, d=64, P=16, scale=0.5),
 }
 
@@ -195,7 +198,8 @@ def test_against_the_definition(name):
 
 
 @pytest.mark.parametrize("name", ["drafted tokens", "a question", "page ends", "as many rows as keys", "page ends, heads of 64", "no key among others", "window",
-                                  "pages that are not there", "many without rows", "sink longer than the sequence"])
+                                  "pages that are not there", "many without rows", "sink longer than the sequence", "single tokens beside a question",
+                                  "rows of no sequence"])
 def test_any_row_hint_gives_a_right_result(name):
     """max_rows chooses the kernel; the row counts on the device are what is computed."""
     c = Case(**CASES[name], seed=3)
