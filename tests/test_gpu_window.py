@@ -150,6 +150,22 @@ def test_a_row_that_is_no_number_stays_alone(n, first, value):
     assert (np.abs(got - want) <= tol)[others].all() and (np.abs(got_z - z) <= tol_z)[others].all()
 
 
+@pytest.mark.parametrize("n", [1, 40])
+def test_more_sequences_than_a_launch_takes(n):
+    """A window of one: each row's output is its own V."""
+    import torch
+    from paper_2506_19651_b200 import binding as pb
+    torch.manual_seed(n)
+    batch, first = 33000, 2
+    s = pb.make_shape(0, 1, 0, 1, 1, 1, 64, batch=batch)
+    q, k, v = (torch.randn((batch, m, 1, 64), device="cuda").to(torch.bfloat16) for m in (n, first + n, first + n))
+    o, lse = torch.zeros_like(q), torch.zeros((batch, 1, n), device="cuda")
+    ws = torch.zeros(pb.pevlm_window_workspace_bytes(s, 1, first, n), dtype=torch.uint8, device="cuda")
+    pb.pevlm_window_attn(s, 1, q, k, v, first, n, first + n, o, lse, ws)
+    assert pb.pevlm_read_status(ws) == (0, 0)
+    assert bool((o == v[:, first:]).all()) and bool(lse.isfinite().all())
+
+
 def test_window_of_everything_is_plain_causal():
     """With a window as long as the sequence the rows are those of the full causal prefill, bit for bit."""
     import torch
