@@ -323,6 +323,22 @@ def test_no_query_and_the_smallest_scale(rows):
     c.check(*c.run())
 
 
+@pytest.mark.parametrize("rows", [[1, 2, 1], [1, 60, 2], [50, 60, 70]])
+def test_the_most_sequences_that_a_table_may_have(rows):
+    """Three of 2^20 have rows: the first, one in the middle and the last."""
+    import torch
+    c = Case([90, 16, 75], rows, 4, 2, 64, 16, seed=8)
+    n, at = 2 ** 20, [0, 500001, 2 ** 20 - 1]
+    table = torch.full((n, c.table.shape[1]), -1, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(n, dtype=torch.int32, device="cuda")
+    counts = torch.zeros(n, dtype=torch.int64, device="cuda")
+    table[at], lens[at], counts[at] = c.table, c.d_lens, torch.tensor(rows, device="cuda")
+    c.table, c.d_lens = table, lens
+    c.start = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), counts.cumsum(0)]).int()
+    c.pages = c.pb.make_pages(c.pages.num_pages, 16, n, table.shape[1])
+    c.check(*c.run())
+
+
 def test_rows_without_lse():
     import torch
     c = Case([100], [2], 4, 2, 64, 16)
