@@ -13,7 +13,7 @@
 // (4.5 TB/s of cache), four tokens 36.5 -> 28.5; 12.5K keys 22.7 -> 11.2; heads of 64 45.9 -> 21.5.  Above 32 rows the
 // tile kernel is the faster one (56 rows at 50K keys: 33.8 us, and it needs no accumulator of rows x head size per warp).
 // Under a sliding window (a form of its own) the pieces are those of the sink and of the window; what lies between is not visited: one token under
-// 4,096 positions beside 64, 28/4 heads: 7.8 us, two launches in a chain.
+// 4,096 positions beside 64, 28/4 heads: 8.0 us, two launches in a chain.
 #include "internal.h"
 #include "ptx.cuh"
 

@@ -24,7 +24,7 @@
 // What bounds it: large batches HBM (64 sequences of up to 16K keys, 28/4 heads: 304 MB at 6 TB/s while the warps are in their loops, 55 of 72 us;
 // the start, the slowest warps, the join and the merge are the rest); small ones the chain lengths -> part -> pages -> tiles -> join -> merge
 // and the instructions (277 of a warp a tile of 16 keys, 128 of them the conversions and the products with the scales; half of the ALU's
-// throughput, which conversions share, is in use).  One token against 50K keys (29 MB) 17.5 us, of which 6 in the loop; 16 sequences of heads of
+// throughput, which conversions share, is in use).  One token against 50K keys (29 MB) 17.8 us, of which 6 in the loop; 16 sequences of heads of
 // 64 under a window (38 MB) 27.8.  Two tiles a step (two chains of dependent products): 116 -> 77.5 us for the 64 sequences.
 #include "packed_list.cuh"
 
