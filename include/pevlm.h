@@ -254,7 +254,7 @@ typedef struct {
  * ceil(lens[r] / page_len) pages are pushed onto the free list, and its length becomes 0.
  *   finished, lens [num_seqs], page_table [num_seqs, max_pages], free_count [1]: read
  *   free_list [num_pages]: written from entry *free_count on; lens_out [num_seqs], free_count_out [1]: written
- * Outputs must not share memory with inputs (PEVLM_EINVAL): a step goes lens -> release -> lens_out -> assign -> lens.  The page table
+ * Outputs must not share memory with inputs or with one another (PEVLM_EINVAL): a step goes lens -> release -> lens_out -> assign -> lens.  The page table
  * stays as it is: what stands behind a sequence's length means nothing.  Lengths and counts outside their range count as the
  * nearest one inside; nothing is written past the end of the free list.
  */
@@ -272,7 +272,7 @@ int pevlm_pages_release(const pevlm_pages_t* pages, const int32_t* finished, con
  *   of pevlm_rope_qk, slots those of pevlm_packed_store, lens_out and row_start those of pevlm_packed_attn.)
  * A sequence whose pages run out (the free list, counted over all sequences up to this one, or its row of the table) or
  * whose rows end past max_rows gets no pages: its rows have slot -1 and its lens_out stays lens.  One that needs no fresh page is never
- * turned away for the list.  Outputs must not be the inputs (see pevlm_pages_release).  max_rows >= 0, <= 2^30.
+ * turned away for the list.  Outputs, the page table among them, must not share memory (see pevlm_pages_release).  max_rows >= 0, <= 2^30.
  */
 int pevlm_pages_assign(const pevlm_pages_t* pages, const int32_t* lens, const int32_t* new_lens, int32_t* page_table,
                        const int32_t* free_list, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out,

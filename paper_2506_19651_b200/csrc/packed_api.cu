@@ -1,5 +1,6 @@
 // C ABI of the calls on a cache of many sequences (pages, 4-bit keys and values): argument checking and launches.
 #include <cstring>
+#include <initializer_list>
 
 #include "internal.h"
 
@@ -20,10 +21,25 @@ static int check_pages(const pevlm_pages_t* g) {
 
 static int page_shift(const pevlm_pages_t* g) { return __builtin_ctz(static_cast<unsigned>(g->page_len)); }
 
-// Whether two arrays of so many int32 share memory.
-static bool overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + 4 * static_cast<uintptr_t>(m) && y < x + 4 * static_cast<uintptr_t>(n);
+// So many int32, and whether two such arrays share memory.
+struct Ints {
+    const int32_t* at;
+    int64_t n;
+};
+static bool overlap(const Ints& a, const Ints& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return a.n > 0 && b.n > 0 && x < y + 4 * static_cast<uintptr_t>(b.n) && y < x + 4 * static_cast<uintptr_t>(a.n);
+}
+
+// Whether an output of a call on pages shares memory with one of its inputs or with another output.  (Every CTA reads all inputs while others write.)
+static bool outputs_shared(std::initializer_list<Ints> outputs, std::initializer_list<Ints> inputs) {
+    for (const Ints* out = outputs.begin(); out != outputs.end(); ++out) {
+        for (const Ints& in : inputs)
+            if (overlap(*out, in)) return true;
+        for (const Ints* other = out + 1; other != outputs.end(); ++other)
+            if (overlap(*out, *other)) return true;
+    }
+    return false;
 }
 
 // What the packed calls ask of a shape.
@@ -50,8 +66,8 @@ int pevlm_pages_release(const pevlm_pages_t* g, const int32_t* finished, const i
     if (!aligned_to(finished, 4) || !aligned_to(lens, 4) || !aligned_to(page_table, 4) || !aligned_to(free_list, 4) ||
         !aligned_to(free_count, 4) || !aligned_to(lens_out, 4) || !aligned_to(free_count_out, 4))
         return PEVLM_EALIGN;
-    if (overlap(lens_out, g->num_seqs, lens, g->num_seqs) || overlap(lens_out, g->num_seqs, finished, g->num_seqs) || overlap(free_count_out, 1, free_count, 1))
-        return PEVLM_EINVAL;
+    const int64_t n = g->num_seqs;
+    if (outputs_shared({{free_list, g->num_pages}, {lens_out, n}, {free_count_out, 1}}, {{finished, n}, {lens, n}, {page_table, n * g->max_pages}, {free_count, 1}})) return PEVLM_EINVAL;
     rc = check_device();
     if (rc != PEVLM_OK) return rc;
     ReleaseParams p{finished, lens, page_table, free_count, free_list, lens_out, free_count_out, g->num_pages, g->num_seqs, g->max_pages, page_shift(g)};
@@ -72,9 +88,9 @@ int pevlm_pages_assign(const pevlm_pages_t* g, const int32_t* lens, const int32_
         !aligned_to(slots, 16) || !aligned_to(positions, 16))
         return PEVLM_EALIGN;
     const int64_t n = g->num_seqs;
-    for (const int32_t* in : {lens, new_lens})
-        if (overlap(lens_out, n, in, n) || overlap(row_start, n + 1, in, n) || overlap(slots, max_rows, in, n) || overlap(positions, max_rows, in, n)) return PEVLM_EINVAL;
-    if (overlap(free_count_out, 1, free_count, 1)) return PEVLM_EINVAL;
+    if (outputs_shared({{page_table, n * g->max_pages}, {lens_out, n}, {free_count_out, 1}, {row_start, n + 1}, {slots, max_rows}, {positions, max_rows}},
+                       {{lens, n}, {new_lens, n}, {free_list, g->num_pages}, {free_count, 1}}))
+        return PEVLM_EINVAL;
     rc = check_device();
     if (rc != PEVLM_OK) return rc;
     AssignParams p{lens, new_lens, free_list, free_count, page_table, lens_out, free_count_out, row_start, slots, positions,
