@@ -279,6 +279,15 @@ int pevlm_pages_assign(const pevlm_pages_t* pages, const int32_t* lens, const in
                        int32_t* row_start, int32_t* slots, int32_t* positions, int64_t max_rows, void* stream);
 
 /*
+ * The same for a step that brings n_rows rows, 0 <= n_rows <= max_rows, whatever new_lens says: a sequence whose rows end past n_rows is
+ * turned away like one whose rows end past max_rows.  (Granted, it would hold tokens that nobody has written, i.e. what the pages'
+ * former sequences left there.)  slots and positions are written up to max_rows all the same.
+ */
+int pevlm_pages_assign_rows(const pevlm_pages_t* pages, const int32_t* lens, const int32_t* new_lens, int32_t* page_table,
+                            const int32_t* free_list, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out,
+                            int32_t* row_start, int32_t* slots, int32_t* positions, int64_t max_rows, int64_t n_rows, void* stream);
+
+/*
  * The packed cache: K and V in groups of 16 values along the head, each value an e2m1 number (4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6
  * and their negatives) times the e4m3 scale of its group; 4.5 bits a value.  For a group with largest magnitude m
  *   scale = e4m3(clamp(m / 6, 2^-9, 448)),  value = e2m1(x / scale), both to nearest, halfway to the even code, the second saturating,

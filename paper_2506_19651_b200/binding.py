@@ -26,7 +26,7 @@ EXPORTS = ["pevlm_rope_qk", "pevlm_rope_qkv", "pevlm_layer_forward", "pevlm_rope
            "pevlm_query_attn_noalloc",
            "pevlm_workspace_bytes", "pevlm_read_status", "pevlm_selftest_wait_expiry", "pevlm_tile_stats", "pevlm_strerror",
            "pevlm_last_cuda_error",
-           "pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_cache_bytes", "pevlm_packed_store", "pevlm_packed_load",
+           "pevlm_pages_release", "pevlm_pages_assign", "pevlm_pages_assign_rows", "pevlm_packed_cache_bytes", "pevlm_packed_store", "pevlm_packed_load",
            "pevlm_packed_attn", "pevlm_packed_workspace_bytes", "pevlm_window_attn", "pevlm_window_workspace_bytes"]
 
 
@@ -103,6 +103,7 @@ def lib():
         l.pevlm_last_cuda_error.restype = C.c_char_p
         l.pevlm_pages_release.argtypes = [gp] + [vp] * 8
         l.pevlm_pages_assign.argtypes = [gp] + [vp] * 10 + [C.c_int64, vp]
+        l.pevlm_pages_assign_rows.argtypes = [gp] + [vp] * 10 + [C.c_int64, C.c_int64, vp]
         l.pevlm_packed_cache_bytes.argtypes = [sp, gp]
         l.pevlm_packed_cache_bytes.restype = C.c_size_t
         l.pevlm_packed_store.argtypes = [sp, gp, vp, vp, C.c_int64, C.c_int64, vp, C.c_int64, vp, vp]
@@ -114,7 +115,7 @@ def lib():
         l.pevlm_window_attn.restype = C.c_int
         l.pevlm_window_workspace_bytes.argtypes = [sp, C.c_int32, C.c_int64, C.c_int64]
         l.pevlm_window_workspace_bytes.restype = C.c_size_t
-        for name in ("pevlm_pages_release", "pevlm_pages_assign", "pevlm_packed_store", "pevlm_packed_load", "pevlm_packed_attn"):
+        for name in ("pevlm_pages_release", "pevlm_pages_assign", "pevlm_pages_assign_rows", "pevlm_packed_store", "pevlm_packed_load", "pevlm_packed_attn"):
             getattr(l, name).restype = C.c_int
         for name in ("pevlm_rope_qk", "pevlm_parallel_prefill_attn", "pevlm_assemble_kv", "pevlm_query_attn",
                      "pevlm_read_status", "pevlm_tile_stats"):
@@ -253,6 +254,12 @@ def pevlm_pages_assign(pages: Pages, lens, new_lens, page_table, free_list, free
                        positions, max_rows: int):
     _check(_native().pages_assign(_pages_address(pages), lens, new_lens, page_table, free_list, free_count, lens_out, free_count_out,
                                   row_start, slots, positions, max_rows, _stream()), "pevlm_pages_assign")
+
+
+def pevlm_pages_assign_rows(pages: Pages, lens, new_lens, page_table, free_list, free_count, lens_out, free_count_out, row_start, slots,
+                            positions, max_rows: int, n_rows: int):
+    _check(_native().pages_assign_rows(_pages_address(pages), lens, new_lens, page_table, free_list, free_count, lens_out, free_count_out,
+                                       row_start, slots, positions, max_rows, n_rows, _stream()), "pevlm_pages_assign_rows")
 
 
 def pevlm_packed_cache_bytes(shape: Shape, pages: Pages) -> int:

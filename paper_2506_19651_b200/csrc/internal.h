@@ -211,7 +211,7 @@ struct CopySegments {
 struct AssignParams {
     const int32_t *lens, *new_lens, *free_list, *free_count;
     int32_t *page_table, *lens_out, *free_count_out, *row_start, *slots, *positions;
-    int64_t max_rows, rows_per_cta;  // rows_per_cta is set by launch_assign
+    int64_t max_rows, n_rows, rows_per_cta;  // n_rows: of the step; rows_per_cta is set by launch_assign
     int32_t num_pages, num_seqs, max_pages, page_shift;
 };
 struct ReleaseParams {

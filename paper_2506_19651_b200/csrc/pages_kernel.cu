@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(THREADS) assign_kernel(const __grid_constant__
         Sums all;
         const Sums to = base + scan<THREADS>(Sums{add, need}, all);
         // Of those that fit their rows, the ones that get pages are all up to some sequence: behind the first that takes the sums past
-        // max_rows or past the free list no later one with new rows (with fresh pages) stays within.  So no page is passed over.
-        const bool granted = there && fits && to.rows <= p.max_rows && (need == 0 || to.pages <= count);
+        // n_rows or past the free list no later one with new rows (with fresh pages) stays within.  So no page is passed over.
+        const bool granted = there && fits && to.rows <= p.n_rows && (need == 0 || to.pages <= count);
         if (blockIdx.x == 0) {
             if (there) {
                 p.lens_out[r] = granted ? len + add : len;

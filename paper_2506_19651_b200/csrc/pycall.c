@@ -109,6 +109,11 @@ BEGIN(pages_assign, 13)
     int64_t rows = I(11); void* st = P(12);
 END(pevlm_pages_assign((const pevlm_pages_t*)s, len, add, tab, fl, fc, lo, fo, rs, sl, ps, rows, st))
 
+BEGIN(pages_assign_rows, 14)
+    void *len = P(1), *add = P(2), *tab = P(3), *fl = P(4), *fc = P(5), *lo = P(6), *fo = P(7), *rs = P(8), *sl = P(9), *ps = P(10);
+    int64_t rows = I(11), brought = I(12); void* st = P(13);
+END(pevlm_pages_assign_rows((const pevlm_pages_t*)s, len, add, tab, fl, fc, lo, fo, rs, sl, ps, rows, brought, st))
+
 BEGIN(packed_store, 10)
     void *g = P(1), *k = P(2), *v = P(3); int64_t ks = I(4), vs = I(5); void* sl = P(6); int64_t rows = I(7); void *c = P(8), *st = P(9);
 END(pevlm_packed_store(s, (const pevlm_pages_t*)g, k, v, ks, vs, sl, rows, c, st))
@@ -125,7 +130,7 @@ END(pevlm_packed_attn(s, (const pevlm_pages_t*)g, (int32_t)window, q, qs, c, tab
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(rope_qk), METHOD(rope_qkv), METHOD(rope_qk_mrope), METHOD(parallel_prefill_attn),
                                 METHOD(block_attn), METHOD(assemble_kv), METHOD(query_attn), METHOD(query_attn_noalloc),
-                                METHOD(layer_forward), METHOD(pages_release), METHOD(pages_assign),
+                                METHOD(layer_forward), METHOD(pages_release), METHOD(pages_assign), METHOD(pages_assign_rows),
                                 METHOD(packed_store), METHOD(packed_load), METHOD(packed_attn),
                                 METHOD(window_attn), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pevlm_call", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -213,7 +213,8 @@ class PackedCache:
     GPU, so a step may be captured into a graph and replayed with whatever `new_lens` and `finished` hold by then.
 
     `max_rows` rows at most a step, of all sequences one after another; `window` > 0 leaves each row the last `window` positions and its
-    sequence's first `sink` ones.  Steps follow one another on one stream: the workspace and the roped rows are the object's.  A sequence that finds no pages keeps its length and its rows get slot -1 (see pevlm_pages_assign)."""
+    sequence's first `sink` ones.  Steps follow one another on one stream: the workspace and the roped rows are the object's.  A sequence that finds no pages, or
+    whose rows are not all among those that the step brings, keeps its length and its rows get slot -1 (see pevlm_pages_assign_rows)."""
 
     def __init__(self, num_seqs, max_tokens, num_pages, page_len, max_rows, Hq, Hkv, d, theta, window=0, sink=0, scale=0.0, device="cuda"):
         import torch
@@ -233,6 +234,7 @@ class PackedCache:
         self.free_count, self._free_count = torch.full((1,), num_pages, dtype=torch.int32, device=device), ints(1)
         self.row_start, self.slots, self.positions = ints(num_seqs + 1), ints(max_rows), ints(max_rows)
         self._none = ints(num_seqs)
+        self._new_lens, self._room = None, 0  # of the last extend()
         self._q, self._k = (torch.empty((max_rows, h, d), dtype=torch.bfloat16, device=device) for h in (Hq, Hkv))
         self._lse = torch.empty(0, dtype=torch.float32, device=device)
         self.workspace = torch.zeros(pb.pevlm_packed_workspace_bytes(self.shape, self.pages, max_rows, max_rows), dtype=torch.uint8, device=device)
@@ -266,21 +268,35 @@ class PackedCache:
             if t is not None and (t.numel() != self.pages.num_seqs or t.dtype is not self.lens.dtype or not t.is_contiguous()):
                 raise ValueError(f"{t.numel()} of {t.dtype} where an int32 for each of {self.pages.num_seqs} sequences is read")
 
-    def extend(self, new_lens, finished=None):
-        """Gives back the pages of the `finished` sequences and makes room for new_lens (int32, on the GPU, one for each sequence) more tokens
-        of each: row_start, slots and positions say where the rows of the step go."""
+    def extend(self, new_lens, finished=None, rows=None):
+        """Gives back the pages of the `finished` sequences and makes room for new_lens (int32, on the GPU, one for each sequence; unchanged until
+        store()) more tokens of each: row_start, slots and positions say where the rows of the step go.  `rows`: as many as store() will bring; a sequence whose
+        rows are not all among them is turned away.  Without it there is room for max_rows, and a store() of fewer makes the page call again."""
+        if rows is not None and not 0 <= rows <= self.max_rows:
+            raise ValueError(f"a step of {rows} rows where at most {self.max_rows} fit")
         self._int_per_sequence(new_lens, finished)
         self._at_hand(new_lens, finished)
         pb.pevlm_pages_release(self.pages, self._none if finished is None else finished, self.lens, self.page_table, self.free_list,
                                self.free_count, self._lens, self._free_count)
-        pb.pevlm_pages_assign(self.pages, self._lens, new_lens, self.page_table, self.free_list, self._free_count, self.lens,
-                              self.free_count, self.row_start, self.slots, self.positions, self.max_rows)
+        self._new_lens = new_lens
+        self._assign(self.max_rows if rows is None else rows)
+
+    def _assign(self, rows):
+        """From the lengths and the free pages between the two page calls of extend(), which the second one leaves as they are."""
+        pb.pevlm_pages_assign_rows(self.pages, self._lens, self._new_lens, self.page_table, self.free_list, self._free_count, self.lens,
+                                   self.free_count, self.row_start, self.slots, self.positions, self.max_rows, rows)
+        self._room = rows
 
     def store(self, k, v):
-        """Rows of roped K and of V [n, Hkv, d] (rows may be strided) into the slots of the last extend()."""
+        """Rows of roped K and of V [n, Hkv, d] (rows may be strided) into the slots of the last extend(): all rows of its step, since a sequence
+        whose rows are not all there is turned away (see extend)."""
         n = self._rows(k, v)
         strides = self._row_stride(k, self.Hkv), self._row_stride(v, self.Hkv)
+        if self._new_lens is not None and n > self._room:
+            raise ValueError(f"{n} rows for a step of {self._room}")
         self._at_hand(k, v)
+        if self._new_lens is not None and n < self._room:
+            self._assign(n)
         pb.pevlm_packed_store(self.shape, self.pages, k, v, self.slots, n, self.cache, *strides)
 
     def attend(self, q, most=None):
@@ -303,7 +319,7 @@ class PackedCache:
             raise ValueError("RoPE reads the rows of q and k one after another")
         self._int_per_sequence(new_lens, finished)
         self._at_hand(q, k, v)
-        self.extend(new_lens, finished)
+        self.extend(new_lens, finished, n)
         if n > 0:
             pb.pevlm_rope_qk(self.shape, q, k, self._q, self._k, 0, n, self.positions)
         self.store(self._k[:n], v)

@@ -66,3 +66,13 @@ def test_side_by_side_is_served():
     pb.pevlm_pages_assign(g, p["lens"], p["new_lens"], p["page_table"], p["free_list"], p["free_count"], p["mid"], p["count_mid"], p["row_start"],
                           p["page_table"], p["page_table"], 0)
     assert p["lens"].tolist() == [3, 0, 17, 1, 2]
+
+
+def test_rows_that_a_step_cannot_bring():
+    pbuild.build()
+    lib, g = pb.lib(), pb.make_pages(NUM_PAGES, 16, SEQS, MAX_PAGES)
+    args = [C.c_void_p(4096 * (i + 1)) for i in range(10)]
+    for room, n in ((ROWS, -1), (ROWS, ROWS + 1), (0, 1), (-1, -1)):
+        assert lib.pevlm_pages_assign_rows(C.byref(g), *args, room, n, None) == pb.PEVLM_EINVAL
+    args[5] = args[0]
+    assert lib.pevlm_pages_assign_rows(C.byref(g), *args, ROWS, ROWS, None) == pb.PEVLM_EINVAL
