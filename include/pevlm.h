@@ -282,10 +282,13 @@ int pevlm_pages_assign(const pevlm_pages_t* pages, const int32_t* lens, const in
  * The same for a step that brings n_rows rows, 0 <= n_rows <= max_rows, whatever new_lens says: a sequence whose rows end past n_rows is
  * turned away like one whose rows end past max_rows.  (Granted, it would hold tokens that nobody has written, i.e. what the pages'
  * former sequences left there.)  slots and positions are written up to max_rows all the same.
+ *   key_lens [num_seqs], may be NULL: lens_out, but 0 for a sequence that was turned away.  As the lens of pevlm_packed_attn it leaves the rows
+ *   of such a sequence without keys: output 0 and LSE -inf, where lens_out would place them at the end of what the sequence held before.
  */
 int pevlm_pages_assign_rows(const pevlm_pages_t* pages, const int32_t* lens, const int32_t* new_lens, int32_t* page_table,
                             const int32_t* free_list, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out,
-                            int32_t* row_start, int32_t* slots, int32_t* positions, int64_t max_rows, int64_t n_rows, void* stream);
+                            int32_t* row_start, int32_t* slots, int32_t* positions, int64_t max_rows, int64_t n_rows, int32_t* key_lens,
+                            void* stream);
 
 /*
  * The packed cache: K and V in groups of 16 values along the head, each value an e2m1 number (4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6

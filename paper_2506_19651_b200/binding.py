@@ -103,7 +103,7 @@ def lib():
         l.pevlm_last_cuda_error.restype = C.c_char_p
         l.pevlm_pages_release.argtypes = [gp] + [vp] * 8
         l.pevlm_pages_assign.argtypes = [gp] + [vp] * 10 + [C.c_int64, vp]
-        l.pevlm_pages_assign_rows.argtypes = [gp] + [vp] * 10 + [C.c_int64, C.c_int64, vp]
+        l.pevlm_pages_assign_rows.argtypes = [gp] + [vp] * 10 + [C.c_int64, C.c_int64, vp, vp]
         l.pevlm_packed_cache_bytes.argtypes = [sp, gp]
         l.pevlm_packed_cache_bytes.restype = C.c_size_t
         l.pevlm_packed_store.argtypes = [sp, gp, vp, vp, C.c_int64, C.c_int64, vp, C.c_int64, vp, vp]
@@ -257,9 +257,9 @@ def pevlm_pages_assign(pages: Pages, lens, new_lens, page_table, free_list, free
 
 
 def pevlm_pages_assign_rows(pages: Pages, lens, new_lens, page_table, free_list, free_count, lens_out, free_count_out, row_start, slots,
-                            positions, max_rows: int, n_rows: int):
+                            positions, max_rows: int, n_rows: int, key_lens=None):
     _check(_native().pages_assign_rows(_pages_address(pages), lens, new_lens, page_table, free_list, free_count, lens_out, free_count_out,
-                                       row_start, slots, positions, max_rows, n_rows, _stream()), "pevlm_pages_assign_rows")
+                                       row_start, slots, positions, max_rows, n_rows, key_lens, _stream()), "pevlm_pages_assign_rows")
 
 
 def pevlm_packed_cache_bytes(shape: Shape, pages: Pages) -> int:

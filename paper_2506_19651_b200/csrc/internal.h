@@ -210,7 +210,7 @@ struct CopySegments {
 // Page tables and slots (pages_kernel.cu).
 struct AssignParams {
     const int32_t *lens, *new_lens, *free_list, *free_count;
-    int32_t *page_table, *lens_out, *free_count_out, *row_start, *slots, *positions;
+    int32_t *page_table, *lens_out, *free_count_out, *row_start, *slots, *positions, *key_lens;  // key_lens: may be NULL
     int64_t max_rows, n_rows, rows_per_cta;  // n_rows: of the step; rows_per_cta is set by launch_assign
     int32_t num_pages, num_seqs, max_pages, page_shift;
 };

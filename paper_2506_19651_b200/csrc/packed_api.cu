@@ -78,12 +78,13 @@ int pevlm_pages_release(const pevlm_pages_t* g, const int32_t* finished, const i
 int pevlm_pages_assign(const pevlm_pages_t* g, const int32_t* lens, const int32_t* new_lens, int32_t* page_table,
                        const int32_t* free_list, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out,
                        int32_t* row_start, int32_t* slots, int32_t* positions, int64_t max_rows, void* stream) {
-    return pevlm_pages_assign_rows(g, lens, new_lens, page_table, free_list, free_count, lens_out, free_count_out, row_start, slots, positions, max_rows, max_rows, stream);
+    return pevlm_pages_assign_rows(g, lens, new_lens, page_table, free_list, free_count, lens_out, free_count_out, row_start, slots, positions, max_rows, max_rows, nullptr, stream);
 }
 
 int pevlm_pages_assign_rows(const pevlm_pages_t* g, const int32_t* lens, const int32_t* new_lens, int32_t* page_table,
                             const int32_t* free_list, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out,
-                            int32_t* row_start, int32_t* slots, int32_t* positions, int64_t max_rows, int64_t n_rows, void* stream) {
+                            int32_t* row_start, int32_t* slots, int32_t* positions, int64_t max_rows, int64_t n_rows, int32_t* key_lens,
+                            void* stream) {
     int rc = check_pages(g);
     if (rc != PEVLM_OK) return rc;
     if (max_rows < 0 || max_rows > 1ll << 30 || n_rows < 0 || n_rows > max_rows) return PEVLM_EINVAL;
@@ -91,15 +92,15 @@ int pevlm_pages_assign_rows(const pevlm_pages_t* g, const int32_t* lens, const i
     if (max_rows > 0 && (!slots || !positions)) return PEVLM_EINVAL;
     if (!aligned_to(lens, 4) || !aligned_to(new_lens, 4) || !aligned_to(page_table, 4) || !aligned_to(free_list, 4) ||
         !aligned_to(free_count, 4) || !aligned_to(lens_out, 4) || !aligned_to(free_count_out, 4) || !aligned_to(row_start, 4) ||
-        !aligned_to(slots, 16) || !aligned_to(positions, 16))
+        !aligned_to(slots, 16) || !aligned_to(positions, 16) || !aligned_to(key_lens, 4))
         return PEVLM_EALIGN;
     const int64_t n = g->num_seqs;
-    if (outputs_shared({{page_table, n * g->max_pages}, {lens_out, n}, {free_count_out, 1}, {row_start, n + 1}, {slots, max_rows}, {positions, max_rows}},
+    if (outputs_shared({{page_table, n * g->max_pages}, {lens_out, n}, {free_count_out, 1}, {row_start, n + 1}, {slots, max_rows}, {positions, max_rows}, {key_lens, key_lens ? n : 0}},
                        {{lens, n}, {new_lens, n}, {free_list, g->num_pages}, {free_count, 1}}))
         return PEVLM_EINVAL;
     rc = check_device();
     if (rc != PEVLM_OK) return rc;
-    AssignParams p{lens, new_lens, free_list, free_count, page_table, lens_out, free_count_out, row_start, slots, positions,
+    AssignParams p{lens, new_lens, free_list, free_count, page_table, lens_out, free_count_out, row_start, slots, positions, key_lens,
                    max_rows, n_rows, 0, g->num_pages, g->num_seqs, g->max_pages, page_shift(g)};
     const cudaError_t e = launch_assign(p, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? PEVLM_OK : cuda_fail(e, "assign launch");

@@ -96,6 +96,7 @@ __global__ void __launch_bounds__(THREADS) assign_kernel(const __grid_constant__
         if (blockIdx.x == 0) {
             if (there) {
                 p.lens_out[r] = granted ? len + add : len;
+                if (p.key_lens) p.key_lens[r] = granted ? len + add : add > 0 ? 0 : len;
                 p.row_start[r + 1] = static_cast<int>(min(to.rows, static_cast<int64_t>(INT32_MAX)));
             }
             if (granted && need > 0) taken = to.pages;

@@ -109,10 +109,10 @@ BEGIN(pages_assign, 13)
     int64_t rows = I(11); void* st = P(12);
 END(pevlm_pages_assign((const pevlm_pages_t*)s, len, add, tab, fl, fc, lo, fo, rs, sl, ps, rows, st))
 
-BEGIN(pages_assign_rows, 14)
+BEGIN(pages_assign_rows, 15)
     void *len = P(1), *add = P(2), *tab = P(3), *fl = P(4), *fc = P(5), *lo = P(6), *fo = P(7), *rs = P(8), *sl = P(9), *ps = P(10);
-    int64_t rows = I(11), brought = I(12); void* st = P(13);
-END(pevlm_pages_assign_rows((const pevlm_pages_t*)s, len, add, tab, fl, fc, lo, fo, rs, sl, ps, rows, brought, st))
+    int64_t rows = I(11), brought = I(12); void *kl = P(13), *st = P(14);
+END(pevlm_pages_assign_rows((const pevlm_pages_t*)s, len, add, tab, fl, fc, lo, fo, rs, sl, ps, rows, brought, kl, st))
 
 BEGIN(packed_store, 10)
     void *g = P(1), *k = P(2), *v = P(3); int64_t ks = I(4), vs = I(5); void* sl = P(6); int64_t rows = I(7); void *c = P(8), *st = P(9);

@@ -214,7 +214,7 @@ class PackedCache:
 
     `max_rows` rows at most a step, of all sequences one after another; `window` > 0 leaves each row the last `window` positions and its
     sequence's first `sink` ones.  Steps follow one another on one stream: the workspace and the roped rows are the object's.  A sequence that finds no pages, or
-    whose rows are not all among those that the step brings, keeps its length and its rows get slot -1 (see pevlm_pages_assign_rows)."""
+    whose rows are not all among those that the step brings, keeps its length; its rows get slot -1, output 0 and LSE -inf (see pevlm_pages_assign_rows)."""
 
     def __init__(self, num_seqs, max_tokens, num_pages, page_len, max_rows, Hq, Hkv, d, theta, window=0, sink=0, scale=0.0, device="cuda"):
         import torch
@@ -231,6 +231,7 @@ class PackedCache:
         self.page_table = torch.full((num_seqs, self.pages.max_pages), -1, dtype=torch.int32, device=device)
         self.free_list = torch.arange(num_pages, dtype=torch.int32, device=device)
         self.lens, self._lens = ints(num_seqs), ints(num_seqs)  # after a step; between its two calls
+        self._key_lens = ints(num_seqs)                         # as attend() takes them: 0 for a sequence that was turned away
         self.free_count, self._free_count = torch.full((1,), num_pages, dtype=torch.int32, device=device), ints(1)
         self.row_start, self.slots, self.positions = ints(num_seqs + 1), ints(max_rows), ints(max_rows)
         self._none = ints(num_seqs)
@@ -284,7 +285,7 @@ class PackedCache:
     def _assign(self, rows):
         """From the lengths and the free pages between the two page calls of extend(), which the second one leaves as they are."""
         pb.pevlm_pages_assign_rows(self.pages, self._lens, self._new_lens, self.page_table, self.free_list, self._free_count, self.lens,
-                                   self.free_count, self.row_start, self.slots, self.positions, self.max_rows, rows)
+                                   self.free_count, self.row_start, self.slots, self.positions, self.max_rows, rows, self._key_lens)
         self._room = rows
 
     def store(self, k, v):
@@ -301,12 +302,12 @@ class PackedCache:
 
     def attend(self, q, most=None):
         """Attention of roped q [n, Hq, d], the rows of the last extend().  `most`: rows of one sequence, if the caller knows (saves two launches).
-        Rows of a sequence that found no room have no meaning.  Returns (o [n,Hq,d], lse [Hq,n])."""
+        Rows of a sequence that was turned away have output 0 and LSE -inf, rows of no sequence are not written.  Returns (o [n,Hq,d], lse [Hq,n])."""
         n = self._rows(q)
         stride = self._row_stride(q, self.Hq)
         self._at_hand(q)
         o, lse = q.new_empty((n, self.Hq, self.d)), self._lse.new_empty((self.Hq, n))
-        pb.pevlm_packed_attn(self.shape, self.pages, self.window, q, self.cache, self.page_table, self.lens, self.row_start, n,
+        pb.pevlm_packed_attn(self.shape, self.pages, self.window, q, self.cache, self.page_table, self._key_lens, self.row_start, n,
                              n if most is None else min(most, n), o, lse, self.workspace, stride)
         return o, lse
 

@@ -103,3 +103,45 @@ def test_all_rows_that_come_are_held():
         c.store(*_rows(5, (2, 2)))
     with pytest.raises(ValueError, match="at most 64 fit"):
         c.extend(_i32([0, 0]), rows=65)
+
+
+@pytest.mark.parametrize("why", ["the free list", "the table", "the room for rows", "rows that do not come"])
+def test_rows_that_were_turned_away_say_so(why):
+    """Output 0 and LSE -inf for all of them, and the right numbers for the others."""
+    import torch
+    from paper_2506_19651_b200.layer import PackedCache
+    make = lambda pages: PackedCache(3, 48, pages, 16, 40, 4, 2, 64, 1e4)
+    c, twin = make(4 if why == "the free list" else 9), make(9)  # 9, 20 and 3 tokens hold four
+    first = _rows(32, seed=5)
+    for x in (c, twin):
+        x.step(*first, _i32([9, 20, 3]))
+    new = {"the free list": [7, 20, 1], "the table": [7, 29, 1], "the room for rows": [7, 2, 32], "rows that do not come": [7, 2, 9]}[why]
+    turned = {"the free list": 1, "the table": 1}.get(why, 2)
+    n = {"the room for rows": 40, "rows that do not come": 15}.get(why, sum(new))
+    q, k, v = _rows(n, seed=6)
+    o, lse = c.step(q, k, v, _i32(new))
+    start = np.concatenate([[0], np.cumsum(new)])
+    rows = torch.zeros(n, dtype=torch.bool, device="cuda")
+    rows[start[turned]:start[turned + 1]] = True
+    assert bool((o[rows] == 0).all()) and bool((lse[:, rows] == -float("inf")).all()) and int(rows.sum()) > 0
+    assert c.lens.tolist() == [x + (0 if r == turned else y) for r, (x, y) in enumerate(zip([9, 20, 3], new))]
+    served = [0 if r == turned else x for r, x in enumerate(new)]
+    want, want_lse = twin.step(*(x[~rows].contiguous() for x in (q, k, v)), _i32(served))
+    # the same rows, shared out among the warps otherwise: two results, each off by the tolerances of test_gpu_packed_attn at most, with |v| <= 8,
+    # sum |q k| * scale <= 16 and |lse| <= 7: 2 (2^-8 |o| + (2^-11 + 2^-22 + 2^-13) 8) and 2 (64 * 2^-24 * 16 + 2^-20 * 8)
+    assert bool(o[~rows].double().sub(want.double()).abs().max() <= 2.0 ** -7 * want.double().abs().max() + 16 * (2.0 ** -11 + 2.0 ** -22 + 2.0 ** -13))
+    assert bool((lse[:, ~rows] - want_lse).abs().max() <= 2.0 ** -13 + 2.0 ** -16)
+    assert bool(torch.isfinite(lse[:, ~rows]).all())
+
+
+def test_key_lengths():
+    """lens_out, 0 for the sequences that are turned away; one without new rows never is."""
+    from paper_2506_19651_b200 import binding as pb
+    g, seqs = pb.make_pages(6, 16, 7, 3), 7
+    lens, new = _i32([5, 16, 40, 0, 33, 48, 20]), _i32([3, 20, 9, 0, 1, 0, 2])
+    for n, want in ((64, [8, 36, 0, 0, 34, 48, 22]), (23, [8, 36, 0, 0, 0, 48, 0])):
+        out, key = _i32([-9] * seqs), _i32([-9] * seqs)
+        pb.pevlm_pages_assign_rows(g, lens, new, _i32(np.zeros((seqs, 3))), _i32(range(6)), _i32([6]), out, _i32([0]), _i32([0] * 8), _i32([0] * 64), _i32([0] * 64),
+                                   64, n, key)
+        assert key.tolist() == want
+        assert out.tolist() == [w or x for w, x in zip(want, lens.tolist())]

@@ -73,6 +73,16 @@ def test_rows_that_a_step_cannot_bring():
     lib, g = pb.lib(), pb.make_pages(NUM_PAGES, 16, SEQS, MAX_PAGES)
     args = [C.c_void_p(4096 * (i + 1)) for i in range(10)]
     for room, n in ((ROWS, -1), (ROWS, ROWS + 1), (0, 1), (-1, -1)):
-        assert lib.pevlm_pages_assign_rows(C.byref(g), *args, room, n, None) == pb.PEVLM_EINVAL
+        assert lib.pevlm_pages_assign_rows(C.byref(g), *args, room, n, None, None) == pb.PEVLM_EINVAL
     args[5] = args[0]
-    assert lib.pevlm_pages_assign_rows(C.byref(g), *args, ROWS, ROWS, None) == pb.PEVLM_EINVAL
+    assert lib.pevlm_pages_assign_rows(C.byref(g), *args, ROWS, ROWS, None, None) == pb.PEVLM_EINVAL
+
+
+def test_key_lens_apart_from_everything():
+    pbuild.build()
+    lib, g = pb.lib(), pb.make_pages(NUM_PAGES, 16, SEQS, MAX_PAGES)
+    args = [C.c_void_p(4096 * (i + 1)) for i in range(10)]
+    for i, (name, n) in enumerate(ASSIGN.items()):
+        for offset in (0, 4 * n - 4, 4 - 4 * SEQS):
+            assert lib.pevlm_pages_assign_rows(C.byref(g), *args, ROWS, ROWS, C.c_void_p(4096 * (i + 1) + offset), None) == pb.PEVLM_EINVAL, name
+    assert lib.pevlm_pages_assign_rows(C.byref(g), *args, ROWS, ROWS, C.c_void_p(2), None) == pb.PEVLM_EALIGN
