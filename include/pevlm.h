@@ -329,7 +329,8 @@ int pevlm_packed_load(const pevlm_shape_t* shape, const pevlm_pages_t* pages, co
  *   pevlm_pages_assign leaves them;  o [n_rows, Hq, d] bf16, lse [Hq, n_rows] fp32 (may be NULL), written
  *   max_rows: most rows of one sequence, as the caller knows it (n_rows if not): chooses the kernels, which takes time if it is far too large; a larger
  *   row count than that stays correct
- * A row that sees no key (a length of 0, or fewer keys than rows) has output 0 and LSE -inf.  Keys in a page whose table entry is outside
+ * A row that sees no key (a length of 0, or fewer keys than rows) has output 0 and LSE -inf; so have those of a sequence whose rows end past
+ * n_rows, i.e. are not all there.  Keys in a page whose table entry is outside
  * [0, num_pages) count as not there, and what keys hold that no row sees (behind the length, in front of the windows) does not matter.  Rows of q that no sequence has are not read, and of o and lse not written.  Scores of finite rows are formed from fp16
  * operands (the cache's values are exact in it) and summed in fp32, probabilities rounded to fp16.
  * workspace: >= pevlm_packed_workspace_bytes(...) bytes, 256-byte aligned, needs no value; two calls at a time need two.

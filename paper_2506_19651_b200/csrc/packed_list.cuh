@@ -26,7 +26,8 @@ struct PackedSeq {
 template <int TS>
 __device__ __forceinline__ PackedSeq packed_seq(const PackedAttnParams& p, int len, int from, int to, int rows_per_chunk) {
     PackedSeq s;
-    s.len = min(max(len, 0), p.max_pages << p.page_shift);
+    // rows that are not all there: where they stand in the sequence would have to be guessed, so they see no key
+    s.len = to > p.n_rows ? 0 : min(max(len, 0), p.max_pages << p.page_shift);
     s.row0 = min(max(from, 0), p.n_rows);
     s.n = max(min(to, p.n_rows) - s.row0, 0);
     if (s.n < p.n_from || s.n > p.n_to) s.n = 0;
