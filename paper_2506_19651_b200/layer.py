@@ -220,6 +220,8 @@ class PackedCache:
         import torch
         if max_rows < 1:
             raise ValueError(f"a step of {max_rows} rows")
+        if not 0 <= window < 2 ** 31:
+            raise ValueError(f"a window of {window} positions")
         self.pages = pb.make_pages(num_pages, page_len, num_seqs, -(-max_tokens // page_len))
         self.shape = pb.make_shape(sink, 1, 0, 1, Hq, Hkv, d, theta=theta, scale=scale)
         n_bytes = pb.pevlm_packed_cache_bytes(self.shape, self.pages)
@@ -238,7 +240,10 @@ class PackedCache:
         self._new_lens, self._room = None, 0  # of the last extend()
         self._q, self._k = (torch.empty((max_rows, h, d), dtype=torch.bfloat16, device=device) for h in (Hq, Hkv))
         self._lse = torch.empty(0, dtype=torch.float32, device=device)
-        self.workspace = torch.zeros(pb.pevlm_packed_workspace_bytes(self.shape, self.pages, max_rows, max_rows), dtype=torch.uint8, device=device)
+        n_bytes = pb.pevlm_packed_workspace_bytes(self.shape, self.pages, max_rows, max_rows)
+        if n_bytes == 0:
+            raise ValueError(f"steps of {max_rows} rows of {Hq}/{Hkv} heads")
+        self.workspace = torch.zeros(n_bytes, dtype=torch.uint8, device=device)
 
     def _rows(self, *tensors):
         n = tensors[0].shape[0]
@@ -263,6 +268,12 @@ class PackedCache:
         if t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.d) or (t.shape[0] > 1 and t.stride(0) < heads * self.d):
             raise ValueError(f"rows with strides {t.stride()}: the {heads} heads of a row have to stand one after another, and rows apart")
         return t.stride(0) if t.shape[0] > 1 else 0
+
+    def _aligned(self, *tensors):
+        """What the calls would refuse only after a page call has been made."""
+        for t in tensors:
+            if t.shape[0] > 0 and (t.data_ptr() % 16 != 0 or t.shape[0] > 1 and t.stride(0) % 8 != 0):
+                raise ValueError(f"rows at {t.data_ptr():#x}, {t.stride(0)} elements apart: they are read 16 bytes at a time")
 
     def _int_per_sequence(self, *tensors):
         for t in tensors:
@@ -295,6 +306,7 @@ class PackedCache:
         strides = self._row_stride(k, self.Hkv), self._row_stride(v, self.Hkv)
         if self._new_lens is not None and n > self._room:
             raise ValueError(f"{n} rows for a step of {self._room}")
+        self._aligned(k, v)
         self._at_hand(k, v)
         if self._new_lens is not None and n < self._room:
             self._assign(n)
@@ -312,12 +324,15 @@ class PackedCache:
         return o, lse
 
     def step(self, q, k, v, new_lens, finished=None, most=None):
-        """One step of the layer from un-roped rows: extend(), RoPE at the rows' positions, store(), attend()."""
+        """One step of the layer from un-roped rows: extend(), RoPE at the rows' positions, store(), attend().  A step that is refused changes nothing."""
         n = self._rows(q, k, v)
         for t, heads in ((q, self.Hq), (k, self.Hkv), (v, self.Hkv)):
             self._row_stride(t, heads)
         if not q.is_contiguous() or not k.is_contiguous():
             raise ValueError("RoPE reads the rows of q and k one after another")
+        self._aligned(q, k, v)
+        if most is not None and most < 0:
+            raise ValueError(f"at most {most} rows of a sequence")
         self._int_per_sequence(new_lens, finished)
         self._at_hand(q, k, v)
         self.extend(new_lens, finished, n)
