@@ -97,7 +97,7 @@ END(pevlm_layer_forward(s, (int32_t)last, q, k, v, qv, qq, kc, vc, ov, (float*)l
 BEGIN(window_attn, 13)
     int64_t window = I(1); void *q = P(2), *k = P(3), *v = P(4); int64_t first = I(5), tokens = I(6), rows = I(7);
     void *o = P(8), *lse = P(9), *ws = P(10); int64_t wb = I(11); void* st = P(12);
-END(pevlm_window_attn(s, (int32_t)window, q, k, v, first, tokens, rows, o, (float*)lse, ws, (size_t)wb, st))
+END(window != (int32_t)window ? PEVLM_EINVAL : pevlm_window_attn(s, (int32_t)window, q, k, v, first, tokens, rows, o, (float*)lse, ws, (size_t)wb, st))
 
 /* The calls on pages: the first argument is the address of a pevlm_pages_t, or of a shape with the pages behind it. */
 BEGIN(pages_release, 9)
@@ -125,7 +125,7 @@ END(pevlm_packed_load(s, (const pevlm_pages_t*)g, c, sl, rows, k, v, st))
 BEGIN(packed_attn, 16)
     void* g = P(1); int64_t window = I(2); void* q = P(3); int64_t qs = I(4); void *c = P(5), *tab = P(6), *len = P(7), *rs = P(8);
     int64_t rows = I(9), most = I(10); void *o = P(11), *lse = P(12), *ws = P(13); int64_t wb = I(14); void* st = P(15);
-END(pevlm_packed_attn(s, (const pevlm_pages_t*)g, (int32_t)window, q, qs, c, tab, len, rs, rows, most, o, (float*)lse, ws, (size_t)wb, st))
+END(window != (int32_t)window ? PEVLM_EINVAL : pevlm_packed_attn(s, (const pevlm_pages_t*)g, (int32_t)window, q, qs, c, tab, len, rs, rows, most, o, (float*)lse, ws, (size_t)wb, st))
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(rope_qk), METHOD(rope_qkv), METHOD(rope_qk_mrope), METHOD(parallel_prefill_attn),
