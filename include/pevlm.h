@@ -332,7 +332,8 @@ int pevlm_packed_load(const pevlm_shape_t* shape, const pevlm_pages_t* pages, co
  * A row that sees no key (a length of 0, or fewer keys than rows) has output 0 and LSE -inf; so have those of a sequence whose rows end past
  * n_rows, i.e. are not all there.  Keys in a page whose table entry is outside
  * [0, num_pages) count as not there, and what keys hold that no row sees (behind the length, in front of the windows) does not matter.  Rows of q that no sequence has are not read, and of o and lse not written.  Scores of finite rows are formed from fp16
- * operands (the cache's values are exact in it) and summed in fp32, probabilities rounded to fp16.
+ * operands (the cache's values are exact in it, and of a row of q what is at least 2^-31 of its largest element; what is smaller is off by 2^-39 of that at
+ * most) and summed in fp32, probabilities rounded to fp16.
  * workspace: >= pevlm_packed_workspace_bytes(...) bytes, 256-byte aligned, needs no value; two calls at a time need two.
  */
 int pevlm_packed_attn(const pevlm_shape_t* shape, const pevlm_pages_t* pages, int32_t window, const void* q, int64_t q_stride,

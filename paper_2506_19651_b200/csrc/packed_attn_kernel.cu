@@ -18,8 +18,8 @@
 // elements 32 t + 4 s .. + 3 of the head (thread t of four; Q's fragments are cut the same way, the order of a sum's terms is
 // free), the rows of V^T are elements 16 g + 2 i, + 1, so a thread needs 16 bytes of codes of two keys, 8 bytes of four, and one scale for
 // all of them.  Probabilities change from the result's layout to the operand's by movmatrix.
-// Rows of Q are scaled by a power of two to at most 2 in magnitude, so that any bf16 values fit fp16 (what is below 2^-24 of the
-// row's largest is lost, as it would be in fp32's rounding of the sum); sums, maxima and outputs are fp32.  Probabilities are rounded to fp16
+// Rows of Q are scaled by a power of two, so that any bf16 values fit fp16: exactly, down to 2^-31 of the row's largest (RowPower in packed_list.cuh;
+// with S in bf16, whose conversions of the keys take three instructions a pair more, the 64 sequences below took 85.7 us); sums, maxima and outputs are fp32.  Probabilities are rounded to fp16
 // (2^-11 of each; 2^-25 of the running reference where smaller).
 // What bounds it: large batches HBM (64 sequences of up to 16K keys, 28/4 heads: 304 MB at 6 TB/s while the warps are in their loops, 55 of 72 us;
 // the start, the slowest warps, the join and the merge are the rest); small ones the chain lengths -> part -> pages -> tiles -> join -> merge
@@ -229,9 +229,8 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                 for (int c = 0; c < KS * 2; ++c) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(x[c] << 16)), fabsf(__uint_as_float(x[c] & 0xffff0000u))));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                // 2^e <= top < 2^(e + 1); down by 2^e, the softmax scale up by it
-                const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23), 1), 253);
-                const float down = __uint_as_float(static_cast<uint32_t>(254 - e) << 23), up = row_scale(e, p.scale_log2);
+                const RowPower power(top);
+                const float down = power.down(), up = power.up(p.scale_log2);
 #pragma unroll
                 for (int c = 0; c < KS * 2; ++c)
                     q[j][c >> 1][c & 1] = pack_f16x2(__uint_as_float(x[c] << 16) * down, __uint_as_float(x[c] & 0xffff0000u) * down);

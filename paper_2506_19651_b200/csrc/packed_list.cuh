@@ -94,11 +94,19 @@ struct PackedPart {
     PackedSeq s;  // that sequence
 };
 
-// Softmax scale, in units of log2, of a row of Q that is held 2^(e - 127) times smaller.  Kept within the normal numbers: the scores it goes with
-// are below 2^21, which makes nothing of the smallest, but -inf of a hidden key times 0 would be no number.
-__device__ __forceinline__ float row_scale(int e, float scale_log2) {
-    return fminf(fmaxf(__uint_as_float(static_cast<uint32_t>(e) << 23) * scale_log2, 1.17549435e-38f), 3.40282347e38f);
-}
+// Rows of Q are held in fp16, scaled by a power of two so that their largest element (of exponent field e) has a magnitude in [2^14, 2^15): what is at
+// least 2^-31 of it is exact then, and what is smaller off by at most 2^-39 of it.  (A score is off by at most 2^-39 max|q| * sum|k| for that, over the
+// keys' elements beside such small ones: visible only where scale * max|q| * sum|k| is some 10^7.)  Sums of 128 products with values up to 2688 are below 2^34.
+struct RowPower {
+    int e;
+    __device__ __forceinline__ explicit RowPower(float top) { e = min(max(static_cast<int>(__float_as_uint(top) >> 23), 15), 254); }
+    __device__ __forceinline__ float down() const { return __uint_as_float(static_cast<uint32_t>(268 - e) << 23); }
+    // Softmax scale, in units of log2, of the row as it is held.  Kept within the normal numbers: the scores it goes with are below 2^34, which makes
+    // nothing of the smallest, but -inf of a hidden key times 0 would be no number.
+    __device__ __forceinline__ float up(float scale_log2) const {
+        return fminf(fmaxf(__uint_as_float(static_cast<uint32_t>(e) << 23) * 0x1p-14f * scale_log2, 1.17549435e-38f), 3.40282347e38f);
+    }
+};
 
 // First sequence from r on that has rows (num_seqs: none has), for a whole warp: 128 are looked at together, since a server's table may hold many
 // that have none in this call.

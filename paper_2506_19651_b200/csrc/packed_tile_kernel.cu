@@ -8,7 +8,7 @@
 //   warps 12, 14 (first CTA of the pair) issue the MMAs, warp 12 of the second hands its feeder's work over; warp 13 fetches the packed tiles (cp.async.bulk, 16 tokens of a page each),
 //   warp 15     makes the work items
 // Everything is fp16 instead of bf16: the cache's values are exact in it and two instructions a pair make them (a conversion and the product
-// with the scale; bf16 would take five); rows of Q are scaled by a power of two (see packed_attn_kernel.cu), whose inverse goes into the row's softmax
+// with the scale; bf16 would take five); rows of Q are scaled by a power of two (RowPower in packed_list.cuh), whose inverse goes into the row's softmax
 // scale; probabilities (at most 2^8 above the reference) keep 11 bits.
 // A row block is 256 rows (token, head of the group), each CTA's 128 against the same keys, so a pair unpacks every tile once for 256 rows; with
 // 4.5 bits a value the cache itself is no bandwidth to speak of.  What bounds it is what bounds attn_kernel.cu: the softmax
@@ -579,7 +579,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
             const int nt = it.nt;
             if (out_k == k) out_end = t + nt;
             started = k + 1;
-            // ---- Q: a row a thread, scaled by a power of two to at most 2
+            // ---- Q: a row a thread, scaled by a power of two
             if (k > 0) wait(bars.q_free, (k - 1) & 1, kTwQFree);
             {
                 const int rr = it.chunk * L::kRows + static_cast<int>(rank) * kTile + row;
@@ -597,9 +597,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                     asm("max.bf16x2 %0, %1, %2;" : "=r"(top2) : "r"(a), "r"(top2));
                 }
                 const float top = fmaxf(__uint_as_float(top2 << 16), __uint_as_float(top2 & 0xffff0000u));
-                const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23), 1), 253);
-                const float down = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
-                s_scale[k & 3][row] = row_scale(e, p.scale_log2);
+                const RowPower power(top);
+                const float down = power.down();
+                s_scale[k & 3][row] = power.up(p.scale_log2);
 #pragma unroll 4
                 for (int c = 0; c < D / 8; ++c) {
                     const uint4 x = some ? src[c] : make_uint4(0u, 0u, 0u, 0u);
