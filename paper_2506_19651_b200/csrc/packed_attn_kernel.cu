@@ -20,7 +20,7 @@
 // all of them.  Probabilities change from the result's layout to the operand's by movmatrix.
 // Rows of Q are scaled by a power of two, so that any bf16 values fit fp16: exactly, down to 2^-31 of the row's largest (RowPower in packed_list.cuh;
 // with S in bf16, whose conversions of the keys take three instructions a pair more, the 64 sequences below took 85.7 us); sums, maxima and outputs are fp32.  Probabilities are rounded to fp16
-// (2^-11 of each; 2^-25 of the running reference where smaller).
+// (2^-11 of each; 2^-32 of the running reference where smaller, see kHeadroom).
 // What bounds it: large batches HBM (64 sequences of up to 16K keys, 28/4 heads: 304 MB at 6 TB/s while the warps are in their loops, 55 of 72 us;
 // the start, the slowest warps, the join and the merge are the rest); small ones the chain lengths -> part -> pages -> tiles -> join -> merge
 // and the instructions (277 of a warp a tile of 16 keys, 128 of them the conversions and the products with the scales; half of the ALU's
@@ -414,15 +414,15 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                             y[x][e] = fmaf(s[j][x][e], sc[j][e & 1], -m[j][e & 1]);
                             most = fmaxf(most, y[x][e]);
                         }
-                    // the reference maximum moves when a score is more than 2^8 above it
-                    if (__any_sync(0xffffffffu, most > 8.f)) {
+                    // m, which stands kHeadroom below the reference maximum, moves when a score is more than 2^8 above that
+                    if (__any_sync(0xffffffffu, most > 8.f + kHeadroom)) {
 #pragma unroll
                         for (int b = 0; b < 2; ++b) {
                             float top = fmaxf(fmaxf(s[j][0][b], s[j][0][2 + b]), fmaxf(s[j][1][b], s[j][1][2 + b])) * sc[j][b];
                             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                            const float to = fmaxf(m[j][b], top), alpha = fast_exp2(m[j][b] - to);
+                            const float to = fmaxf(m[j][b], top - kHeadroom), alpha = fast_exp2(m[j][b] - to);
                             m[j][b] = to;
                             l[j][b] *= alpha;
 #pragma unroll

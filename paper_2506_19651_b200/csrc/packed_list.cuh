@@ -108,6 +108,10 @@ struct RowPower {
     }
 };
 
+// Probabilities are formed 2^kHeadroom times larger than the softmax of the running reference has them (the row sums with them, so that it cancels): with the
+// reference up to 2^8 below the largest they are at most 2^15, and what fp16 loses of the smallest is 2^-32 of the reference instead of 2^-25.
+constexpr float kHeadroom = 7.f;
+
 // First sequence from r on that has rows (num_seqs: none has), for a whole warp: 128 are looked at together, since a server's table may hold many
 // that have none in this call.
 __device__ __forceinline__ int seq_with_rows(const PackedAttnParams& p, int r) {

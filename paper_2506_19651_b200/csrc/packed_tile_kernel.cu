@@ -9,7 +9,7 @@
 //   warp 15     makes the work items
 // Everything is fp16 instead of bf16: the cache's values are exact in it and two instructions a pair make them (a conversion and the product
 // with the scale; bf16 would take five); rows of Q are scaled by a power of two (RowPower in packed_list.cuh), whose inverse goes into the row's softmax
-// scale; probabilities (at most 2^8 above the reference) keep 11 bits.
+// scale; probabilities (at most 2^8 above the reference, and raised by kHeadroom) keep 11 bits.
 // A row block is 256 rows (token, head of the group), each CTA's 128 against the same keys, so a pair unpacks every tile once for 256 rows; with
 // 4.5 bits a value the cache itself is no bandwidth to speak of.  What bounds it is what bounds attn_kernel.cu: the softmax
 // beside running MMAs, and the power of the tensor cores: 256 tokens of 28/4 heads against 74K keys take 254 us back to back at the power cap (1,070
@@ -453,7 +453,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                 __syncwarp();
             }
             if (row_ok) {
-                const float m_log2 = m == -INFINITY ? kNoMax : m * scale;
+                const float m_log2 = m == -INFINITY ? kNoMax : m * scale - kHeadroom;
                 if (!done.whole) {
                     share[L::kRows * D + in_unit] = m_log2;
                     share[L::kRows * (D + 1) + in_unit] = l;
@@ -728,7 +728,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                 }
                 if (t >= 2) wait_pv_done(t - 2, kTwPFree);
                 if (t > 0) turn_wait(kPassTurn, wg, quarter);
-                const float neg_ms = (m_ref == -INFINITY) ? 0.f : -m_ref * scale;
+                const float neg_ms = (m_ref == -INFINITY) ? 0.f : fmaf(-m_ref, scale, kHeadroom);
                 const uint64_t scale2 = pack_f32x2(scale, scale);
                 const uint64_t shift2 = pack_f32x2(neg_ms, neg_ms);
                 uint64_t sm2[4] = {0ull, 0ull, 0ull, 0ull};
