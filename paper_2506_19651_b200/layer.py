@@ -235,7 +235,7 @@ class PackedCache:
         self.lens, self._lens = ints(num_seqs), ints(num_seqs)  # after a step; between its two calls
         self._key_lens = ints(num_seqs)                         # as attend() takes them: 0 for a sequence that was turned away
         self.free_count, self._free_count = torch.full((1,), num_pages, dtype=torch.int32, device=device), ints(1)
-        self.row_start, self.slots, self.positions = ints(num_seqs + 1), ints(max_rows), ints(max_rows)
+        self.row_start, self.slots, self.positions = ints(num_seqs + 1), ints(max_rows) - 1, ints(max_rows)
         self._none = ints(num_seqs)
         self._new_lens, self._room = None, 0  # of the last extend()
         self._q, self._k = (torch.empty((max_rows, h, d), dtype=torch.bfloat16, device=device) for h in (Hq, Hkv))

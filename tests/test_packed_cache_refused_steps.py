@@ -75,3 +75,11 @@ def test_nothing_changes():
         assert all(torch.equal(a, b) for a, b in zip(before, state()))
     o, lse = c.step(*_rows(17, "cuda"), i32([0, 17]), i32([1, 0]))
     assert c.lens.tolist() == [0, 27] and bool(torch.isfinite(lse).all())
+
+
+def test_no_slots_before_the_first_step():
+    """A store() that no extend() has made room for would put all its rows into the first slot of the first page."""
+    from paper_2506_19651_b200 import build, layer
+    build.build()
+    c = layer.PackedCache(2, 100, 14, 16, 8, 4, 2, 64, 1e4, device="cpu")
+    assert c.slots.tolist() == [-1] * 8 and str(c.slots.dtype) == "torch.int32"
