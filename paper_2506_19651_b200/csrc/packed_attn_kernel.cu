@@ -66,6 +66,7 @@ __device__ __forceinline__ PackedPart my_part(const PackedAttnParams& p, int row
             mine += seq_tiles<4>(p, s[i]);
             upto[i] = mine;
         }
+        __syncwarp();  // the table, for all lanes
         const int64_t to = warp_inclusive(mine), from = to - mine;
         PackedPart part{PackedDeal(__shfl_sync(0xffffffffu, to, 31), gridDim.x * W), 0, 0, s[0]};
         const int64_t lo = part.deal.start(me);
