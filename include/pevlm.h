@@ -295,7 +295,7 @@ int pevlm_pages_assign_rows(const pevlm_pages_t* pages, const int32_t* lens, con
  * and their negatives) times the e4m3 scale of its group; 4.5 bits a value.  For a group with largest magnitude m
  *   scale = e4m3(clamp(m / 6, 2^-9, 448)),  value = e2m1(x / scale), both to nearest, halfway to the even code, the second saturating,
  * so values up to 2688 are in range, and those of a group below 2^-9 * 6 share the smallest scale.  Every value of the cache is a
- * bf16 and an fp16 number: reading it back rounds nothing.
+ * bf16 and an fp16 number: reading it back rounds nothing.  (The sign of a zero is left open: a value that rounds to 0 may be stored as either of the two codes.)
  *   cache [num_pages, Hkv, page_len / 16, 18 * d] bytes: per 16 tokens ("tile") of a page and kv head, token u = 8 h + k, element e:
  *     K codes   byte u * d/2 + e/2                             (element 2i in the low half of its byte)
  *     V codes   byte 8 d + ((h * 8 + c) * 8 + k) * d/16 + b      byte b of eighth c of the head (d/8 elements)
@@ -324,7 +324,8 @@ int pevlm_packed_load(const pevlm_shape_t* shape, const pevlm_pages_t* pages, co
  * Attention of the last rows of every sequence over the packed cache [Eq. 5 for many sequences; single tokens, drafted tokens and
  * question blocks in one call].  Sequence r has lens[r] keys in the cache and rows row_start[r] .. row_start[r + 1] - 1 of q; its i-th
  * of n rows is its token lens[r] - n + i, whose own key is in the cache already, and sees the keys up to its own.  With window > 0
- * only those of the last `window` positions (its own among them) and of the sequence's first sink_len tokens (shape); window = 0: all.
+ * only those of the last `window` positions (its own among them) and of the sequence's first sink_len tokens (shape); window = 0: all.  (A window bounds
+ * what a row reads, not what a sequence holds: pages in front of it go back with the sequence's others, pevlm_pages_release.)
  *   q [n_rows, Hq, d] bf16 roped, rows q_stride elements apart (0 = Hq * d); lens [num_seqs], row_start [num_seqs + 1], page_table: as
  *   pevlm_pages_assign leaves them;  o [n_rows, Hq, d] bf16, lse [Hq, n_rows] fp32 (may be NULL), written
  *   max_rows: most rows of one sequence, as the caller knows it (n_rows if not): chooses the kernels, which takes time if it is far too large; a larger
