@@ -237,7 +237,7 @@ class PackedCache:
         self.free_count, self._free_count = torch.full((1,), num_pages, dtype=torch.int32, device=device), ints(1)
         self.row_start, self.slots, self.positions = ints(num_seqs + 1), ints(max_rows) - 1, ints(max_rows)
         self._none = ints(num_seqs)
-        self._new_lens, self._room = None, 0  # of the last extend()
+        self._room = None  # rows of the last extend()
         self._q, self._k = (torch.empty((max_rows, h, d), dtype=torch.bfloat16, device=device) for h in (Hq, Hkv))
         self._lse = torch.empty(0, dtype=torch.float32, device=device)
         n_bytes = pb.pevlm_packed_workspace_bytes(self.shape, self.pages, max_rows, max_rows)
@@ -281,8 +281,8 @@ class PackedCache:
                 raise ValueError(f"{t.numel()} of {t.dtype} where an int32 for each of {self.pages.num_seqs} sequences is read")
 
     def extend(self, new_lens, finished=None, rows=None):
-        """Gives back the pages of the `finished` sequences and makes room for new_lens (int32, on the GPU, one for each sequence; unchanged until
-        store()) more tokens of each: row_start, slots and positions say where the rows of the step go; they have to be stored before anything attends to them.  `rows`: as many as store() will bring; a sequence whose
+        """Gives back the pages of the `finished` sequences and makes room for new_lens (int32, on the GPU, one for each sequence) more tokens
+        of each: row_start, slots and positions say where the rows of the step go; they have to be stored before anything attends to them.  `rows`: as many as store() will bring; a sequence whose
         rows are not all among them is turned away.  Without it there is room for max_rows, and a store() of fewer makes the page call again."""
         if rows is not None and not 0 <= rows <= self.max_rows:
             raise ValueError(f"a step of {rows} rows where at most {self.max_rows} fit")
@@ -290,12 +290,11 @@ class PackedCache:
         self._at_hand(new_lens, finished)
         pb.pevlm_pages_release(self.pages, self._none if finished is None else finished, self.lens, self.page_table, self.free_list,
                                self.free_count, self._lens, self._free_count)
-        self._new_lens = new_lens
-        self._assign(self.max_rows if rows is None else rows)
+        self._assign(new_lens, self.max_rows if rows is None else rows)
 
-    def _assign(self, rows):
+    def _assign(self, new_lens, rows):
         """From the lengths and the free pages between the two page calls of extend(), which the second one leaves as they are."""
-        pb.pevlm_pages_assign_rows(self.pages, self._lens, self._new_lens, self.page_table, self.free_list, self._free_count, self.lens,
+        pb.pevlm_pages_assign_rows(self.pages, self._lens, new_lens, self.page_table, self.free_list, self._free_count, self.lens,
                                    self.free_count, self.row_start, self.slots, self.positions, self.max_rows, rows, self._key_lens)
         self._room = rows
 
@@ -304,12 +303,12 @@ class PackedCache:
         whose rows are not all there is turned away (see extend)."""
         n = self._rows(k, v)
         strides = self._row_stride(k, self.Hkv), self._row_stride(v, self.Hkv)
-        if self._new_lens is not None and n > self._room:
+        if self._room is not None and n > self._room:
             raise ValueError(f"{n} rows for a step of {self._room}")
         self._aligned(k, v)
         self._at_hand(k, v)
-        if self._new_lens is not None and n < self._room:
-            self._assign(n)
+        if self._room is not None and n < self._room:
+            self._assign(self.row_start.diff(), n)  # row_start has kept the new lengths
         pb.pevlm_packed_store(self.shape, self.pages, k, v, self.slots, n, self.cache, *strides)
 
     def attend(self, q, most=None):

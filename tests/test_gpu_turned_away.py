@@ -145,3 +145,27 @@ def test_key_lengths():
                                    64, n, key)
         assert key.tolist() == want
         assert out.tolist() == [w or x for w, x in zip(want, lens.tolist())]
+
+
+@pytest.mark.parametrize("new", [[3, 5, 0], [0, 5, 9], [-2, 8, 1], [2 ** 31 - 1, 4, 2 ** 31 - 1]])
+def test_new_lengths_may_be_gone_by_the_time_the_rows_come(new):
+    """extend() has read them: a store() of fewer rows goes by what it kept."""
+    from paper_2506_19651_b200.layer import PackedCache
+    make = lambda: PackedCache(3, 64, 12, 16, 40, 4, 2, 64, 1e4)
+    c, twin = make(), make()
+    first, rows = _rows(12, (2, 2), 7), _rows(8, (2, 2), 8)
+    for x in (c, twin):
+        x.extend(_i32([4, 4, 4]), rows=12)
+        x.store(*first)
+    lens = _i32(new)
+    c.extend(lens)
+    lens.zero_()
+    c.store(*rows)
+    twin.extend(_i32(new), rows=8)
+    twin.store(*rows)
+    for name in ("lens", "free_count", "slots", "positions"):
+        assert getattr(c, name).tolist() == getattr(twin, name).tolist(), name
+    # of the sequences that have rows in the step (starts past 2^31 are cut off, so that those behind have no rows at all in one of them)
+    has = [start < 8 for start in c.row_start.tolist()[:3]]
+    for name in ("row_start", "_key_lens"):
+        assert [x for x, h in zip(getattr(c, name).tolist(), has) if h] == [x for x, h in zip(getattr(twin, name).tolist(), has) if h], name

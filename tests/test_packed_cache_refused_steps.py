@@ -46,7 +46,7 @@ def test_before_any_call(monkeypatch):
     for bad in _bad_steps(*_rows(2, "cpu")):
         with pytest.raises(ValueError, match="16 bytes at a time|at most -1 rows"):
             c.step(new_lens=lens, **bad)
-    c._new_lens, c._room = lens, 8  # as extend() leaves it: store() of fewer rows would make the page call again
+    c._room = 8  # as extend() leaves it: store() of fewer rows would make the page call again
     for bad in list(_bad_steps(*_rows(2, "cpu")))[1:4]:
         with pytest.raises(ValueError, match="16 bytes at a time"):
             c.store(bad["k"], bad["v"])
