@@ -662,7 +662,8 @@ static cudaError_t launch_rows(const PackedAttnParams& p, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     // Few units have many shares each (a unit alone those of all CTAs): ten of a row in flight, whose registers leave a CTA to an SM, i.e. two rounds
     // of them.  Many units have two or three: five, and one round.  Measured, ten against five: one token against 50K keys 17.5 / 18.1 us, 64 sequences
-    // of up to 16K 75.0 / 72.5.  (8 rows as a whole with two turns 18.9 and 16 rows in halves with four 30.7 us for 16 sequences under a
+    // of up to 16K 75.0 / 72.5, 4 sequences of 12K 17.6 / 16.9, one with rows among 1,000 of a table 20.5 / 20.9: the rule goes by the table, since which of its sequences have rows
+    // only the GPU knows, and is worth half a microsecond either way.  (8 rows as a whole with two turns 18.9 and 16 rows in halves with four 30.7 us for 16 sequences under a
     // window, as a whole with one turn 27.4.)
     if (NT == 2) return launch_chained<packed_merge_kernel<D, 16, 16, 1, 10>>(dim3(kNumSms - 1), 512, 0, stream, p);
     if (static_cast<int64_t>(p.num_seqs) * p.Hkv <= 32) return launch_chained<packed_merge_kernel<D, 8, 4, 4, 10>>(dim3(kNumSms - 1, 2), 512, 0, stream, p);

@@ -204,7 +204,8 @@ __global__ void __launch_bounds__(THREADS) release_kernel(const __grid_constant_
     if (blockIdx.x == 0 && tid == 0) *p.free_count_out = static_cast<int>(min(count + base.pages, static_cast<int64_t>(p.num_pages)));
 }
 
-// Few sequences and rows: CTAs of 128 threads, whose barriers and sums take less (64 sequences, one row each: both calls 4.5 us, 7.9 with 1,024 threads of four rows).
+// Few sequences and rows: CTAs of 128 threads, whose barriers and sums take less.  Both calls on the GPU, 128 against 1,024 threads of four rows: 1 sequence of one row
+// 3.3 / 5.1 us, 64 of one 3.9 / 6.6, 128 of one 3.9 / 7.0, 128 of four 6.1 / 6.2, 64 of 32 rows 13.7 / 6.0, 512 of one 9.2 / 7.2, 1,024 of one 15.8 / 7.6.
 cudaError_t launch_assign(AssignParams p, cudaStream_t stream) {
     if (p.num_seqs <= 128 && p.max_rows <= 512) {
         p.rows_per_cta = p.max_rows;
