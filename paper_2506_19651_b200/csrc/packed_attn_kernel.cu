@@ -442,8 +442,8 @@ __global__ void __launch_bounds__(PackedAttnLayout<D, NT>::kWarps * 32, 1) packe
                     for (int x = 0; x < 2; ++x) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[x][e] = fast_exp2(y[x][e]);
-                        pb[j][x][0] = transposed(pack_f16x2(y[x][0], y[x][1]));
-                        pb[j][x][1] = transposed(pack_f16x2(y[x][2], y[x][3]));
+                        pb[j][x][0] = transposed(pack_probabilities(y[x][0], y[x][1]));
+                        pb[j][x][1] = transposed(pack_probabilities(y[x][2], y[x][3]));
                     }
                     l[j][0] += (y[0][0] + y[0][2]) + (y[1][0] + y[1][2]);
                     l[j][1] += (y[0][1] + y[0][3]) + (y[1][1] + y[1][3]);

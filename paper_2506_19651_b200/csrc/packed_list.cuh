@@ -203,6 +203,13 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// The same of probabilities: at most 2^15 by kHeadroom, unless scores are so large (2^25 and more in units of log2) that their own rounding moves them by
+// whole powers of two.  Then the largest number there is, where an infinity would make the row no number.
+__device__ __forceinline__ uint32_t pack_probabilities(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 
 // Where row rr (of a sequence and kv head: token rr / G, head rr % G of the group) of the result goes.
 struct PackedRow {

@@ -740,7 +740,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1) pac
                     unpack_f32x2(t2, e0, e1);
                     const float p0 = fast_exp2(e0), p1 = fast_exp2(e1);
                     sm2[i & 3] = add_f32x2(sm2[i & 3], pack_f32x2(p0, p1));
-                    pk[i] = pack_f16x2(p0, p1);
+                    pk[i] = pack_probabilities(p0, p1);
                     if (i % 16 == 15) tmem_st16(tP + i - 15, &pk[i - 15]);
                     if (i == kTileTurn) turn_pass(kPassTurn, wg, quarter);
                 }
