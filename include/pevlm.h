@@ -269,7 +269,8 @@ int pevlm_pages_release(const pevlm_pages_t* pages, const int32_t* finished, con
  *   lens_out [num_seqs] = lens + new_lens, free_count_out [1]
  *   row_start [num_seqs + 1]: first row of each sequence, and the number of rows at the end
  *   slots, positions [max_rows]: written in full, rows that no sequence has with slot -1 and position 0.  (positions is the pos_ids
- *   of pevlm_rope_qk, slots those of pevlm_packed_store, lens_out and row_start those of pevlm_packed_attn.)
+ *   of pevlm_rope_qk, slots those of pevlm_packed_store, lens_out and row_start those of pevlm_packed_attn; where a
+ *   sequence may be turned away, key_lens of pevlm_pages_assign_rows in place of lens_out.)
  * A sequence whose pages run out (the free list, counted over all sequences up to this one, or its row of the table) or
  * whose rows end past max_rows gets no pages: its rows have slot -1 and its lens_out stays lens.  One that needs no fresh page is never
  * turned away for the list.  Outputs, the page table among them, must not share memory (see pevlm_pages_release).  max_rows >= 0, <= 2^30.

@@ -288,6 +288,7 @@ class PackedCache:
             raise ValueError(f"a step of {rows} rows where at most {self.max_rows} fit")
         self._int_per_sequence(new_lens, finished)
         self._at_hand(new_lens, finished)
+        self._room = 0  # nothing to store should one of the two calls be refused
         pb.pevlm_pages_release(self.pages, self._none if finished is None else finished, self.lens, self.page_table, self.free_list,
                                self.free_count, self._lens, self._free_count)
         self._assign(new_lens, self.max_rows if rows is None else rows)

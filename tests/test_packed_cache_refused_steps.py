@@ -83,3 +83,22 @@ def test_no_slots_before_the_first_step():
     build.build()
     c = layer.PackedCache(2, 100, 14, 16, 8, 4, 2, 64, 1e4, device="cpu")
     assert c.slots.tolist() == [-1] * 8 and str(c.slots.dtype) == "torch.int32"
+
+
+@pytest.mark.gpu
+def test_nothing_to_store_behind_a_refused_extend():
+    """New lengths that are the cache's own: refused by the second page call, and the rows of the step before cannot be stored once more."""
+    import torch
+    from paper_2506_19651_b200 import binding as pb
+    from paper_2506_19651_b200.layer import PackedCache
+    c = PackedCache(2, 100, 14, 16, 40, 4, 2, 64, 1e4)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    c.extend(i32([7, 2]))
+    with pytest.raises(pb.PevlmError):
+        c.extend(c.lens)
+    with pytest.raises(ValueError, match="for a step of 0"):
+        c.store(*_rows(9, "cuda")[1:])
+    assert c.lens.tolist() == [7, 2]
+    c.extend(i32([1, 1]))
+    c.store(*_rows(2, "cuda")[1:])
+    assert c.lens.tolist() == [8, 3] and int(c.free_count) == 12
